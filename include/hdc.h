@@ -22,13 +22,14 @@
  *   - N == 0 is a successful no-op.  A context may be used from one host thread at a
  *     time.  Work of one context on different streams may overlap only where it shares no
  *     device scratch of the context:
- *       hdc_search, hdc_pack, hdc_unpack, hdc_hsum, hdc_binarize_classical and
+ *       hdc_search, hdc_pack, hdc_unpack, hdc_hsum, hdc_binarize_classical, hdc_quantize,
+ *       hdc_dequantize, hdc_search_quantized, hdc_product_quantized and
  *       hdc_binarize_online use none and may overlap with anything (so the search of one
  *       chunk of a stream can run beside the encoding of the next);
  *       hdc_encode and hdc_encode_sparse share the encoders' staging buffers: one at a time;
  *       hdc_train_classical and hdc_vsum share the training scratch: one at a time;
- *       hdc_train_online, hdc_train_online_batched and hdc_search_cosine share theirs: one
- *       at a time.
+ *       hdc_train_online, hdc_train_online_batched, hdc_train_online_quantized and
+ *       hdc_search_cosine share theirs: one at a time.
  *     With profiling on (hdc_profile_enable) no two calls may overlap.  A second context of
  *     the same model gives a second set of every buffer.
  */
@@ -246,6 +247,71 @@ int hdc_search_cosine(hdc_ctx *ctx, const uint32_t *hv_dev, int64_t N, const flo
                       float *cos_dev, int32_t *pred_dev, void *stream);
 
 /*
+ * Class rows in 4 bits, between the bits of hdc_binarize_* and the fp32 rows of hdc_search_cosine:
+ * microscaled floats, a scale to every 32 dimensions.  A row of D dimensions has W blocks; block w is
+ * dimensions 32 w .. 32 w + 31, word w of a hypervector.
+ *   scales [N][W]     one byte s a block: 2^(s - 127); 255: the block is no number
+ *   codes  [N][W][4]  32-bit words, 16-byte aligned: nibble j of word r is dimension 32 w + 4 j + r;
+ *                     bit 3 its sign, bits 0-2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Codes of dimensions
+ *                     past D are 0 in every table the caller passes and every one the library writes.
+ *   norm   [N]        fp64 squared norm of a row: the sum of the squares of the values it stands for,
+ *                     not a number where a block is none
+ * 4.25 bits a dimension: rows passed on to another program are these three arrays and D.
+ *
+ * hdc_quantize: with A the largest magnitude of a block, 2^e = 2^max(floor(log2 A) - 2, -127), and every
+ * element x becomes the value nearest to x / 2^e, halfway between two the one whose code is even, beyond
+ * 6 (A / 2^e is below 8) 6; the sign of x is kept.  A block of zeros has s = 0.  A block with an element
+ * that is infinite or no number has s = 255 and codes 0.
+ *   rows_dev [N][D] fp32 (the class rows of a context, or any other), norm_dev may be NULL.
+ * hdc_dequantize: the values, rows_dev [N][D] fp32 out (beyond fp32, which s = 253 and 254 allow but
+ * hdc_quantize never gives, infinite; a block of s = 255 no numbers).
+ * Neither reads C of the context; all matrices are row-major, rows back to back.
+ */
+int hdc_quantize(hdc_ctx *ctx, const float *rows_dev, int64_t N, uint32_t *codes_dev, uint8_t *scales_dev,
+                 double *norm_dev, void *stream);
+int hdc_dequantize(hdc_ctx *ctx, const uint32_t *codes_dev, const uint8_t *scales_dev, int64_t N, float *rows_dev,
+                   void *stream);
+
+/*
+ * hdc_search_cosine against quantised class rows v[C][D]: with s = 2*hv[n] - 1,
+ *   cos[n][c] = <v[c], s> / (sqrt(norm[c]) * sqrt(D))   (0 where norm[c] is 0; fp64),
+ *   pred[n]   = lowest c with the largest cos[n][c]     (compared in fp64; a cosine that is no number
+ *               is below all others, class 0 if all are).
+ * The products of 32 dimensions are whole numbers; their sums are formed without rounding where they
+ * fit 24 bits and in fp64 otherwise.
+ *   hv_dev [N][W] (pad bits zero or not), codes_dev [C][W][4], scales_dev [C][W], norm_dev [C] as hdc_quantize
+ *   leaves them, cos_dev [N][C] fp32 out or NULL, pred_dev [N] int32 out (required).
+ */
+int hdc_search_quantized(hdc_ctx *ctx, const uint32_t *hv_dev, int64_t N, const uint32_t *codes_dev,
+                         const uint8_t *scales_dev, const double *norm_dev, float *cos_dev, int32_t *pred_dev,
+                         void *stream);
+
+/*
+ * Products of quantised rows with one another (class rows of one model with those of another,
+ * real-valued queries with class rows): out[m][n] = <a[m], b[n]>, fp32 sums.
+ *   a_codes_dev [M][W][4], a_scales_dev [M][W], b_codes_dev [N][W][4], b_scales_dev [N][W],
+ *   out_dev [M][N] fp32 out.  M == 0 or N == 0 is a successful no-op.  a and b may be the same rows.
+ */
+int hdc_product_quantized(hdc_ctx *ctx, const uint32_t *a_codes_dev, const uint8_t *a_scales_dev, int64_t M,
+                          const uint32_t *b_codes_dev, const uint8_t *b_scales_dev, int64_t N, float *out_dev,
+                          void *stream);
+
+/*
+ * hdc_train_online_batched for a model that will answer with quantised rows: before every batch the
+ * rows are quantised as by hdc_quantize, the samples of the batch are scored against the quantised rows
+ * (cos_c of hdc_search_quantized, pred and the two fp32 weights as there), and the update goes to
+ * the fp32 rows unchanged: acc[c] = float(double(acc[c]) + delta[c]).  After the last batch codes_dev,
+ * scales_dev and norm_dev (NULL if not wanted) hold the rows as they are then, quantised.
+ *   acc_dev [C][D] fp32 in/out, codes_dev [C][W][4], scales_dev [C][W], norm_dev [C] out (and used
+ *   in between).  N == 0 or epochs == 0 leaves all four as they are.
+ * Other arguments, labels outside [0, C), allocation and scratch are those of hdc_train_online_batched
+ * (hdc_reserve with HDC_RESERVE_ONLINE_BATCHED covers both).
+ */
+int hdc_train_online_quantized(hdc_ctx *ctx, const uint32_t *hv_dev, const int32_t *labels_dev, int64_t N,
+                               int32_t epochs, float lr, int64_t batch, float *acc_dev, uint32_t *codes_dev,
+                               uint8_t *scales_dev, double *norm_dev, void *stream);
+
+/*
  * The stand-alone hypervector primitives of Sec. IV-B.  D and W are the context's.
  *   hdc_pack   (IV-B1)  bits_dev [N][D] bytes (any non-zero byte is a 1) -> hv_dev [N][W],
  *                       LSB first, pad bits 0.
@@ -325,7 +391,10 @@ typedef enum {
     HDC_K_ENCODE_WIDE = 8,     /* the contraction form of hdc_encode for long streams (jobs of 64 or 128 samples) */
     HDC_K_ONLINE_WIDE = 9,     /* the calls among those of HDC_K_ONLINE whose blocks are walked as a whole, one entry a call */
     HDC_K_ONLINE_SPREAD = 10,  /* the calls of both online trainers that go in blocks of up to 2048 samples, one entry a call */
-    HDC_K_COUNT = 11
+    HDC_K_QUANTIZE_ROWS = 11,    /* rows to 4-bit floats, also within hdc_train_online_quantized */
+    HDC_K_SEARCH_QUANTIZED = 12, /* hdc_search_quantized, one entry a call */
+    HDC_K_PRODUCT_QUANTIZED = 13, /* hdc_product_quantized, one entry a call */
+    HDC_K_COUNT = 14
 } hdc_kernel_id;
 #define HDC_PROFILE_SLOTS 512
 int hdc_profile_enable(hdc_ctx *ctx, int enable);

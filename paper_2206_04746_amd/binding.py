@@ -24,12 +24,14 @@ HDC_F32, HDC_U8 = 0, 1
 # every symbol include/hdc.h declares
 SYMBOLS = ["hdc_create", "hdc_destroy", "hdc_encode", "hdc_encode_sparse", "hdc_train_classical",
            "hdc_binarize_classical", "hdc_train_online", "hdc_train_online_batched", "hdc_binarize_online", "hdc_search",
-           "hdc_search_cosine", "hdc_pack", "hdc_unpack", "hdc_hsum", "hdc_vsum", "hdc_vsum_static", "hdc_encoded_words", "hdc_set_label_check", "hdc_reserve",
+           "hdc_search_cosine", "hdc_quantize", "hdc_dequantize", "hdc_search_quantized", "hdc_product_quantized",
+           "hdc_train_online_quantized", "hdc_pack", "hdc_unpack", "hdc_hsum", "hdc_vsum", "hdc_vsum_static", "hdc_encoded_words", "hdc_set_label_check", "hdc_reserve",
            "hdc_profile_enable", "hdc_profile_read",
            "hdc_strerror", "hdc_last_hip_error", "hdc_version"]
 
 KERNEL_IDS = {"encode": 0, "quantize": 1, "accumulate": 2, "online": 3, "search": 4,
-              "online_fwd": 5, "online_bwd": 6, "encode_contract": 7, "encode_wide": 8, "online_wide": 9, "online_spread": 10}
+              "online_fwd": 5, "online_bwd": 6, "encode_contract": 7, "encode_wide": 8, "online_wide": 9, "online_spread": 10,
+              "quantize_rows": 11, "search_quantized": 12, "product_quantized": 13}
 
 
 class HdcParams(ctypes.Structure):
@@ -60,6 +62,11 @@ def _load() -> ctypes.CDLL:
     lib.hdc_train_online_batched.argtypes = [vp, vp, vp, i64, i32, ctypes.c_float, i64, vp, vp]
     lib.hdc_binarize_online.argtypes = [vp, vp, vp, vp]
     lib.hdc_search_cosine.argtypes = [vp, vp, i64, vp, vp, vp, vp]
+    lib.hdc_quantize.argtypes = [vp, vp, i64, vp, vp, vp, vp]
+    lib.hdc_dequantize.argtypes = [vp, vp, vp, i64, vp, vp]
+    lib.hdc_search_quantized.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp, vp]
+    lib.hdc_product_quantized.argtypes = [vp, vp, vp, i64, vp, vp, i64, vp, vp]
+    lib.hdc_train_online_quantized.argtypes = [vp, vp, vp, i64, i32, ctypes.c_float, i64, vp, vp, vp, vp, vp]
     lib.hdc_encoded_words.argtypes = [vp]
     lib.hdc_encoded_words.restype = ctypes.c_int32
     for name in ("hdc_pack", "hdc_unpack", "hdc_hsum", "hdc_vsum"):
@@ -79,7 +86,8 @@ def _load() -> ctypes.CDLL:
     for name in ("hdc_create", "hdc_destroy", "hdc_encode", "hdc_encode_sparse", "hdc_train_classical",
                  "hdc_binarize_classical", "hdc_train_online", "hdc_train_online_batched",
                  "hdc_binarize_online", "hdc_search", "hdc_search_cosine", "hdc_pack", "hdc_unpack",
-                 "hdc_hsum", "hdc_vsum"):
+                 "hdc_hsum", "hdc_vsum", "hdc_quantize", "hdc_dequantize", "hdc_search_quantized",
+                 "hdc_product_quantized", "hdc_train_online_quantized"):
         getattr(lib, name).restype = ctypes.c_int
     lib.hdc_strerror.argtypes = [ctypes.c_int]
     lib.hdc_strerror.restype = ctypes.c_char_p
@@ -213,6 +221,42 @@ class Context:
                                      _dev(acc, torch.float32, (self.C, self.D)),
                                      None if cos is None else _dev(cos, torch.float32, (N, self.C)),
                                      _dev(pred, torch.int32, (N,)), _stream(stream)))
+
+    # Rows of 4-bit floats: codes int32 [N][4 W], scales uint8 [N][W], squared norms float64 [N].
+    def _quantized(self, codes, scales, N):
+        return _dev(codes, torch.int32, (N, 4 * self.W)), _dev(scales, torch.uint8, (N, self.W))
+
+    def hdc_quantize(self, rows, codes, scales, norm=None, stream=None) -> None:
+        N = rows.shape[0]
+        _check(lib.hdc_quantize(self._h, _dev(rows, torch.float32, (N, self.D)), N, *self._quantized(codes, scales, N),
+                                _dev(norm, torch.float64, (N,)), _stream(stream)))
+
+    def hdc_dequantize(self, codes, scales, rows, stream=None) -> None:
+        N = rows.shape[0]
+        _check(lib.hdc_dequantize(self._h, *self._quantized(codes, scales, N), N,
+                                  _dev(rows, torch.float32, (N, self.D)), _stream(stream)))
+
+    def hdc_search_quantized(self, hv, codes, scales, norm, pred, cos=None, stream=None) -> None:
+        N = hv.shape[0]
+        _check(lib.hdc_search_quantized(self._h, _dev(hv, torch.int32, (N, self.W)), N,
+                                        *self._quantized(codes, scales, self.C), _dev(norm, torch.float64, (self.C,)),
+                                        _dev(cos, torch.float32, (N, self.C)), _dev(pred, torch.int32, (N,)),
+                                        _stream(stream)))
+
+    def hdc_product_quantized(self, a_codes, a_scales, b_codes, b_scales, out, stream=None) -> None:
+        M, N = a_codes.shape[0], b_codes.shape[0]
+        _check(lib.hdc_product_quantized(self._h, *self._quantized(a_codes, a_scales, M), M,
+                                         *self._quantized(b_codes, b_scales, N), N,
+                                         _dev(out, torch.float32, (M, N)), _stream(stream)))
+
+    def hdc_train_online_quantized(self, hv, labels, acc, codes, scales, norm, batch: int, epochs: int = 1,
+                                   lr: float = 1.0, stream=None) -> None:
+        N = hv.shape[0]
+        _check(lib.hdc_train_online_quantized(self._h, _dev(hv, torch.int32, (N, self.W)),
+                                              _dev(labels, torch.int32, (N,)), N, int(epochs), float(lr), int(batch),
+                                              _dev(acc, torch.float32, (self.C, self.D)),
+                                              *self._quantized(codes, scales, self.C),
+                                              _dev(norm, torch.float64, (self.C,)), _stream(stream)))
 
     def hdc_pack(self, bits, hv, stream=None) -> None:
         N = bits.shape[0]

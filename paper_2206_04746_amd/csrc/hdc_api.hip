@@ -338,6 +338,7 @@ static int labels_ok(hdc_ctx_impl *c, const int32_t *labels, int64_t N, hipStrea
 static inline hdc_ctx_impl *impl(hdc_ctx *c) { return reinterpret_cast<hdc_ctx_impl *>(c); }
 static inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 static inline bool aligned8(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+static inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace hdc
 
@@ -436,6 +437,49 @@ int hdc_search_cosine(hdc_ctx *ctx, const uint32_t *hv_dev, int64_t N, const flo
     if (!hv_dev || !acc_dev || !pred_dev) return HDC_EINVAL;
     if (!aligned4(hv_dev) || !aligned4(acc_dev) || !aligned4(cos_dev) || !aligned4(pred_dev)) return HDC_EINVAL;
     return launch_search_cosine(impl(ctx), hv_dev, N, acc_dev, cos_dev, pred_dev, static_cast<hipStream_t>(stream));
+}
+
+int hdc_quantize(hdc_ctx *ctx, const float *rows_dev, int64_t N, uint32_t *codes_dev, uint8_t *scales_dev, double *norm_dev, void *stream) {
+    if (!ctx || N < 0) return HDC_EINVAL;
+    if (N == 0) return HDC_OK;
+    if (!rows_dev || !codes_dev || !scales_dev || !aligned4(rows_dev) || !aligned16(codes_dev) || !aligned8(norm_dev)) return HDC_EINVAL;
+    return launch_quantize(impl(ctx), rows_dev, N, codes_dev, scales_dev, norm_dev, nullptr, static_cast<hipStream_t>(stream));
+}
+
+int hdc_dequantize(hdc_ctx *ctx, const uint32_t *codes_dev, const uint8_t *scales_dev, int64_t N, float *rows_dev, void *stream) {
+    if (!ctx || N < 0) return HDC_EINVAL;
+    if (N == 0) return HDC_OK;
+    if (!codes_dev || !scales_dev || !rows_dev || !aligned16(codes_dev) || !aligned4(rows_dev)) return HDC_EINVAL;
+    return launch_dequantize(impl(ctx), codes_dev, scales_dev, N, rows_dev, static_cast<hipStream_t>(stream));
+}
+
+int hdc_search_quantized(hdc_ctx *ctx, const uint32_t *hv_dev, int64_t N, const uint32_t *codes_dev, const uint8_t *scales_dev,
+                         const double *norm_dev, float *cos_dev, int32_t *pred_dev, void *stream) {
+    if (!ctx || N < 0) return HDC_EINVAL;
+    if (N == 0) return HDC_OK;
+    if (!hv_dev || !codes_dev || !scales_dev || !norm_dev || !pred_dev) return HDC_EINVAL;
+    if (!aligned4(hv_dev) || !aligned16(codes_dev) || !aligned8(norm_dev) || !aligned4(cos_dev) || !aligned4(pred_dev)) return HDC_EINVAL;
+    return launch_search_quantized(impl(ctx), hv_dev, N, codes_dev, scales_dev, norm_dev, cos_dev, pred_dev, static_cast<hipStream_t>(stream));
+}
+
+int hdc_product_quantized(hdc_ctx *ctx, const uint32_t *a_codes_dev, const uint8_t *a_scales_dev, int64_t M, const uint32_t *b_codes_dev,
+                          const uint8_t *b_scales_dev, int64_t N, float *out_dev, void *stream) {
+    if (!ctx || M < 0 || N < 0) return HDC_EINVAL;
+    if (M == 0 || N == 0) return HDC_OK;
+    if (!a_codes_dev || !a_scales_dev || !b_codes_dev || !b_scales_dev || !out_dev) return HDC_EINVAL;
+    if (!aligned16(a_codes_dev) || !aligned16(b_codes_dev) || !aligned4(out_dev)) return HDC_EINVAL;
+    return launch_product_quantized(impl(ctx), a_codes_dev, a_scales_dev, M, b_codes_dev, b_scales_dev, N, out_dev, static_cast<hipStream_t>(stream));
+}
+
+int hdc_train_online_quantized(hdc_ctx *ctx, const uint32_t *hv_dev, const int32_t *labels_dev, int64_t N, int32_t epochs, float lr,
+                               int64_t batch, float *acc_dev, uint32_t *codes_dev, uint8_t *scales_dev, double *norm_dev, void *stream) {
+    if (!ctx || N < 0 || epochs < 0 || batch < 1) return HDC_EINVAL;
+    if (N == 0 || epochs == 0) return HDC_OK;
+    if (!hv_dev || !labels_dev || !acc_dev || !codes_dev || !scales_dev) return HDC_EINVAL;
+    if (!aligned4(hv_dev) || !aligned4(labels_dev) || !aligned4(acc_dev) || !aligned16(codes_dev) || !aligned8(norm_dev)) return HDC_EINVAL;
+    if (const int rc = labels_ok(impl(ctx), labels_dev, N, static_cast<hipStream_t>(stream))) return rc;
+    return launch_train_online_quantized(impl(ctx), hv_dev, labels_dev, N, epochs, lr, batch, acc_dev, codes_dev, scales_dev, norm_dev,
+                                         static_cast<hipStream_t>(stream));
 }
 
 int hdc_pack(hdc_ctx *ctx, const uint8_t *bits_dev, int64_t N, uint32_t *hv_dev, void *stream) {

@@ -221,6 +221,18 @@ int launch_train_online_batched(hdc_ctx_impl *c, const uint32_t *hv, const int32
 int launch_binarize_online(hdc_ctx_impl *c, const float *acc, uint32_t *class_hv, hipStream_t s);
 int launch_search_cosine(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const float *acc, float *cos_out,
                          int32_t *pred, hipStream_t s);
+// Rows of 4-bit floats (quantized.hip).  `part`, if not null: the squared-norm partials [N][ceil(D/64)] in place of the norms.
+int launch_quantize(hdc_ctx_impl *c, const float *rows, int64_t N, uint32_t *codes, uint8_t *scales, double *norm, double *part, hipStream_t s);
+int launch_dequantize(hdc_ctx_impl *c, const uint32_t *codes, const uint8_t *scales, int64_t N, float *rows, hipStream_t s);
+int launch_search_quantized(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
+                            float *cos_out, int32_t *pred, hipStream_t s);
+// Partial dot products [*slices][nb][C] of samples with the context's classes.
+int launch_quantized_dots(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const uint32_t *codes, const uint8_t *scales, double *part, int *slices,
+                          hipStream_t s);
+int launch_product_quantized(hdc_ctx_impl *c, const uint32_t *a, const uint8_t *sa, int64_t M, const uint32_t *b, const uint8_t *sb, int64_t N, float *out,
+                             hipStream_t s);
+int launch_train_online_quantized(hdc_ctx_impl *c, const uint32_t *hv, const int32_t *labels, int64_t N, int32_t epochs, float lr, int64_t batch,
+                                  float *acc, uint32_t *codes, uint8_t *scales, double *norm, hipStream_t s);
 int launch_pack(hdc_ctx_impl *c, const uint8_t *bits, int64_t N, uint32_t *hv, hipStream_t s);
 int launch_unpack(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, uint8_t *bits, hipStream_t s);
 int launch_hsum(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, int32_t *out, hipStream_t s);

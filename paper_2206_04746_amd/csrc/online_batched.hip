@@ -1031,31 +1031,24 @@ int reserve_search_cosine(hdc_ctx_impl *c, int64_t queries) {
     return rc;
 }
 
-int launch_train_online_batched(hdc_ctx_impl *c, const uint32_t *hv, const int32_t *labels, int64_t N,
-                                int32_t epochs, float lr, int64_t batch, float *acc, hipStream_t s) {
+// The rows that a call answers with in 4 bits (hdc_train_online_quantized).
+struct QuantRows {
+    uint32_t *codes;
+    uint8_t *scales;
+};
+
+// Batch after batch, each in pieces; `quant`, if not null, has the rows quantised before each and the samples scored against those.
+static int train_pieces(hdc_ctx_impl *c, const uint32_t *hv, const int32_t *labels, int64_t N, int32_t epochs, float lr, int64_t batch,
+                        float *acc, const QuantRows *quant, hipStream_t s) {
     const int C = c->p.C, D = c->p.D, W = c->W;
     const int G = (D + kWave - 1) / kWave;
-    if (batch > N) batch = N;
-    int rc = HDC_OK;
-    const bool pays = online_chain_pays(c, N, batch);
-    if ((pays || online_spread_pays(c, N, batch)) && online_chain_ready(c, s, &rc) && (pays || online_spread_takes(c, N, lr, batch, false))) {
-        // a shorter call with the same batch goes in pieces: their scratch, too, belongs to this call
-        if (batch > c->ob_blocks_batch && !stream_captured(s)) {
-            rc = reserve_pieces(c, batch);
-            if (rc != HDC_OK && rc != HDC_ENOMEM) return rc;
-            c->ob_blocks_batch = batch;
-        }
-        return launch_online_chain(c, hv, labels, N, epochs, lr, batch, false, acc, s);
-    }
-    if (rc != HDC_OK) return rc;
-
     // A batch is worked off in pieces of at most `sb` samples (forward, weights, backward each);
     // sb bounds the scratch: partial dot products and transposed masks.
     const int64_t sb = fwd_sub_batch(C, D, batch);
     const int cb = bwd_dense_width(C);
-    rc = reserve_pieces(c, batch);
+    int rc = reserve_pieces(c, batch);
     if (rc != HDC_OK) return rc;
-    (void)online_chain_ready(c, s, &rc);   // (a longer call, or smaller batches, go in blocks)
+    if (!quant) (void)online_chain_ready(c, s, &rc);   // (a longer call, or smaller batches, go in blocks)
     if (rc != HDC_OK) return rc;
     if (!c->ob_attr_set) {
         const void *kernels[] = {reinterpret_cast<const void *>(online_bwd_kernel<0>),
@@ -1069,18 +1062,21 @@ int launch_train_online_batched(hdc_ctx_impl *c, const uint32_t *hv, const int32
         c->ob_attr_set = true;
     }
 
-    rc = launch_norm(c, acc, G, s);   // squared norms of the rows as handed in
+    if (!quant) rc = launch_norm(c, acc, G, s);   // squared norms of the rows as handed in
     if (rc != HDC_OK) return rc;
     const double root_d = sqrt((double)D);
     const int ttiles = (G + kTileGroups - 1) / kTileGroups;
     for (int32_t e = 0; e < epochs; ++e)
         for (int64_t b0 = 0; b0 < N; b0 += batch) {
             const int64_t B = b0 + batch < N ? batch : N - b0;
+            if (quant) rc = launch_quantize(c, acc, C, quant->codes, quant->scales, nullptr, c->ob_norm_d, s);
+            if (rc != HDC_OK) return rc;
             for (int64_t s0 = 0; s0 < B; s0 += sb) {
                 const int64_t nb = s0 + sb < B ? sb : B - s0;
                 const uint32_t *rows = hv + (b0 + s0) * W;
                 int slices;
-                rc = launch_fwd(c, rows, nb, acc, false, &slices, s);
+                rc = quant ? launch_quantized_dots(c, rows, nb, quant->codes, quant->scales, c->ob_part_d, &slices, s)
+                           : launch_fwd(c, rows, nb, acc, false, &slices, s);
                 if (rc != HDC_OK) return rc;
                 const int64_t ld_used = (nb + kTileSamples - 1) / kTileSamples * kTileSamples;
                 const int cp = cosine_group(C);
@@ -1099,6 +1095,31 @@ int launch_train_online_batched(hdc_ctx_impl *c, const uint32_t *hv, const int32
             }
         }
     return HDC_OK;
+}
+
+int launch_train_online_batched(hdc_ctx_impl *c, const uint32_t *hv, const int32_t *labels, int64_t N,
+                                int32_t epochs, float lr, int64_t batch, float *acc, hipStream_t s) {
+    if (batch > N) batch = N;
+    int rc = HDC_OK;
+    const bool pays = online_chain_pays(c, N, batch);
+    if ((pays || online_spread_pays(c, N, batch)) && online_chain_ready(c, s, &rc) && (pays || online_spread_takes(c, N, lr, batch, false))) {
+        // a shorter call with the same batch goes in pieces: their scratch, too, belongs to this call
+        if (batch > c->ob_blocks_batch && !stream_captured(s)) {
+            rc = reserve_pieces(c, batch);
+            if (rc != HDC_OK && rc != HDC_ENOMEM) return rc;
+            c->ob_blocks_batch = batch;
+        }
+        return launch_online_chain(c, hv, labels, N, epochs, lr, batch, false, acc, s);
+    }
+    if (rc != HDC_OK) return rc;
+    return train_pieces(c, hv, labels, N, epochs, lr, batch, acc, nullptr, s);
+}
+
+int launch_train_online_quantized(hdc_ctx_impl *c, const uint32_t *hv, const int32_t *labels, int64_t N, int32_t epochs, float lr, int64_t batch,
+                                  float *acc, uint32_t *codes, uint8_t *scales, double *norm, hipStream_t s) {
+    const QuantRows quant = {codes, scales};
+    const int rc = train_pieces(c, hv, labels, N, epochs, lr, std::min(batch, N), acc, &quant, s);
+    return rc != HDC_OK ? rc : launch_quantize(c, acc, c->p.C, codes, scales, norm, nullptr, s);
 }
 
 int launch_search_cosine(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const float *acc, float *cos_out,

@@ -23,13 +23,14 @@
  *     time.  Work of one context on different streams may overlap only where it shares no
  *     device scratch of the context:
  *       hdc_search, hdc_pack, hdc_unpack, hdc_hsum, hdc_binarize_classical, hdc_quantize,
- *       hdc_dequantize, hdc_search_quantized, hdc_product_quantized and
+ *       hdc_dequantize, hdc_product_quantized and
  *       hdc_binarize_online use none and may overlap with anything (so the search of one
  *       chunk of a stream can run beside the encoding of the next);
  *       hdc_encode and hdc_encode_sparse share the encoders' staging buffers: one at a time;
  *       hdc_train_classical and hdc_vsum share the training scratch: one at a time;
  *       hdc_train_online, hdc_train_online_batched, hdc_train_online_quantized and
- *       hdc_search_cosine share theirs: one at a time.
+ *       hdc_search_cosine share theirs: one at a time;
+ *       hdc_search_quantized has scratch of its own: one at a time.
  *     With profiling on (hdc_profile_enable) no two calls may overlap.  A second context of
  *     the same model gives a second set of every buffer.
  */

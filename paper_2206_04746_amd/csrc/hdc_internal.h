@@ -117,6 +117,10 @@ struct hdc_ctx_impl {
     int *os_state_d;      // [2] workgroups that have begun (zero between calls), slots in use
     bool os_attr_set[4];  // dynamic-LDS limit of online_spread_kernel raised, by variant
 
+    // hdc_search_quantized: the nearest classes of groups of classes that different blocks search (quantized_search.hip).
+    double *qs_cos_d;
+    int *qs_class_d;
+
     // hdc_encode_sparse (allocated and derived on its first call)
     bool sp_ready;
     uint32_t *sp_b_d;       // [slices][Fp][64] item ^ level 0 (of the compact tables when `compact`)
@@ -226,6 +230,7 @@ int launch_quantize(hdc_ctx_impl *c, const float *rows, int64_t N, uint32_t *cod
 int launch_dequantize(hdc_ctx_impl *c, const uint32_t *codes, const uint8_t *scales, int64_t N, float *rows, hipStream_t s);
 int launch_search_quantized(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
                             float *cos_out, int32_t *pred, hipStream_t s);
+int64_t search_quantized_entries(const hdc_ctx_impl *c);   // of qs_cos_d and qs_class_d
 // Partial dot products [*slices][nb][C] of samples with the context's classes.
 int launch_quantized_dots(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const uint32_t *codes, const uint8_t *scales, double *part, int *slices,
                           hipStream_t s);

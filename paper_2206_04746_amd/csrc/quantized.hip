@@ -1,4 +1,4 @@
-// Class rows in 4-bit floats: quantisation and its way back, cosine inference and products (arXiv 2206.04746, Sec. III, with rows between
+// Class rows in 4-bit floats: quantisation and its way back, and products (arXiv 2206.04746, Sec. III, with rows between
 // the bits of hdc_binarize_online and the 32-bit floats of hdc_search_cosine).
 #include <algorithm>
 
@@ -76,42 +76,6 @@ __global__ __launch_bounds__(256) void dequantize_rows_kernel(const uint32_t *__
         }
 }
 
-// Scalar product of a word of a hypervector with a block of codes, in halves.
-__device__ __forceinline__ int block_halves(uint32_t bits, const uint32_t *code) {
-    int sum = 0;
-    for (int i = 0; i < 32; ++i) {
-        const int v = code_signed_halves(code[i & 3] >> (i & ~3));
-        sum += bits >> i & 1 ? v : -v;
-    }
-    return sum;
-}
-
-// A wave a sample: the products of blocks are whole numbers, summed in fp64.
-__global__ __launch_bounds__(256) void search_quantized_kernel(const uint32_t *__restrict__ hv, int64_t N, int D, int W, int C,
-                                                               const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales,
-                                                               const double *__restrict__ norm, double root_d, double *__restrict__ part,
-                                                               float *__restrict__ cos_out, int32_t *__restrict__ pred_out) {
-    const int lane = threadIdx.x & 63;
-    for (int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); n < N; n += (int64_t)gridDim.x * 4) {
-        double best = 0.0;
-        int pred = -1;
-        for (int c = 0; c < C; ++c) {
-            double dot = 0.0;
-            for (int w = lane; w < W; w += kWave)
-                dot += block_halves(hv[n * W + w], codes + ((int64_t)c * W + w) * 4) * (0.5 * scale_value(scales[(int64_t)c * W + w]));
-            dot = wave_sum(dot);
-            if (part) {
-                if (lane == 0) part[n * C + c] = dot;
-                continue;
-            }
-            const double cs = norm[c] == 0.0 ? 0.0 : dot / (sqrt(norm[c]) * root_d);
-            if (lane == 0 && cos_out) cos_out[n * C + c] = (float)cs;
-            if (cs == cs && (pred < 0 || cs > best)) best = cs, pred = c;
-        }
-        if (lane == 0 && pred_out) pred_out[n] = max(pred, 0);
-    }
-}
-
 // A wave a product of two rows.
 __global__ __launch_bounds__(256) void product_quantized_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
                                                                 const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb, int64_t N, int W,
@@ -145,24 +109,6 @@ int launch_quantize(hdc_ctx_impl *c, const float *rows, int64_t N, uint32_t *cod
 
 int launch_dequantize(hdc_ctx_impl *c, const uint32_t *codes, const uint8_t *scales, int64_t N, float *rows, hipStream_t s) {
     hipLaunchKernelGGL(dequantize_rows_kernel, dim3((unsigned)std::min<int64_t>(N, 1 << 20)), dim3(256), 0, s, codes, scales, N, c->p.D, c->W, rows);
-    HDC_HIP(hipGetLastError());
-    return HDC_OK;
-}
-
-int launch_search_quantized(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
-                            float *cos_out, int32_t *pred, hipStream_t s) {
-    ProfScope prof(c, HDC_K_SEARCH_QUANTIZED, s);
-    hipLaunchKernelGGL(search_quantized_kernel, dim3((unsigned)std::min<int64_t>((N + 3) / 4, 1 << 20)), dim3(256), 0, s, hv, N, c->p.D, c->W, c->p.C, codes,
-                       scales, norm, sqrt((double)c->p.D), static_cast<double *>(nullptr), cos_out, pred);
-    HDC_HIP(hipGetLastError());
-    return HDC_OK;
-}
-
-int launch_quantized_dots(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const uint32_t *codes, const uint8_t *scales, double *part, int *slices,
-                          hipStream_t s) {
-    *slices = 1;
-    hipLaunchKernelGGL(search_quantized_kernel, dim3((unsigned)std::min<int64_t>((nb + 3) / 4, 1 << 20)), dim3(256), 0, s, hv, nb, c->p.D, c->W, c->p.C, codes,
-                       scales, static_cast<const double *>(nullptr), 1.0, part, static_cast<float *>(nullptr), static_cast<int32_t *>(nullptr));
     HDC_HIP(hipGetLastError());
     return HDC_OK;
 }

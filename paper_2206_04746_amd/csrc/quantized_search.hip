@@ -1,0 +1,319 @@
+// Cosine inference with class rows of 4-bit floats (arXiv 2206.04746, Sec. III), and the dot products of online training with them.
+//
+// The matrix cores take such rows as they are, with their scales (v_mfma_scale_f32_32x32x64_f8f6f4), and a sample's bits as +-1 in the
+// same format.  A block of eight waves takes 32 classes and walks over the samples, 32 at a time; each wave has an eighth of the
+// dimensions and holds the codes of its classes there in registers, so that all there is to read on the way is the samples, once.
+// The waves' parts of the dot products meet in LDS.
+//
+// Sums without rounding: the products of a wave are whole multiples of half the smallest scale, and 2 kSteps blocks of 32 dimensions give
+// at most 384 kSteps of the largest (32 times 6).  Where a row's scales within a wave's dimensions lie no further apart than
+// 2^kRange, that fits the 24 bits of the sums.  Where they lie further apart, the blocks are taken in several passes, each of the scales
+// that lie within such a range, and the passes are added in fp64.
+#include <algorithm>
+
+#include "online_weight.h"
+#include "quantized.h"
+
+namespace hdc {
+
+namespace {
+
+constexpr int kWaves = 8, kThreads = kWaves * kWave, kTile = 32;   // classes, samples
+constexpr int kMaxTiles = 32;                                      // of samples a block walks over once for every group of classes
+constexpr int kNoClass = 0x7FFFFFFF;
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+// kSteps: matrix instructions of a wave, 64 dimensions each (a word of either half of the lanes).  Largest difference of scales.
+constexpr int range_of(int steps) {
+    int r = 0;
+    while ((int64_t)steps * 2 * 32 * 6 * 2 << (r + 1) <= 1 << 24) ++r;
+    return r;
+}
+
+template <int B>
+__device__ __forceinline__ v16f mfma(v4u a, v4u b, v16f c, uint32_t scale) {
+    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, B, (int)scale, 0, 0x7F7F7F7F);
+}
+
+// +-1 of a word's 32 dimensions in the order of the codes: 2 is the code of 1, 10 that of -1.
+__device__ __forceinline__ v4u signs_of(uint32_t word) {
+    v4u out;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) out[r] = ((word << (3 - r)) & 0x88888888u) ^ 0xAAAAAAAAu;
+    return out;
+}
+
+// The same number, of which the compiler does not know that it is: what is computed from it is computed here, and not kept in registers
+// from before a loop.
+template <typename T>
+__device__ __forceinline__ T anew(T v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+struct Best {
+    double cos;
+    int c;
+};
+__device__ __forceinline__ Best better(Best a, Best b) { return b.cos > a.cos || (b.cos == a.cos && b.c < a.c) ? b : a; }
+
+// grid (runs of `tiles` tiles of samples, splits of the groups of 32 classes).  kPart: part[n][C] takes the dot products; otherwise
+// cos_out (or null) the cosines, and the nearest class of a block's own goes to pred_out or, if that is null, to best_cos and best_c
+// [split][N].
+template <int kSteps, bool kPart>
+__global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uint32_t *__restrict__ hv, int64_t N, int W, int C,
+                                                                       const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales,
+                                                                       const double *__restrict__ norm, double root_d, int tiles, int groups,
+                                                                       double *__restrict__ part, float *__restrict__ cos_out,
+                                                                       int32_t *__restrict__ pred_out, double *__restrict__ best_cos, int *__restrict__ best_c) {
+    constexpr int kRange = range_of(kSteps), kBlocks = kWaves * 2 * kSteps;   // of a row at a time
+    __shared__ float sums[2][kWaves][kTile][kTile + 1];
+    __shared__ double units[kWaves][kTile];
+    __shared__ int passes_of[kWaves];
+    __shared__ double near_cos[kWaves][kTile];
+    __shared__ int near_c[kWaves][kTile];
+    __shared__ double run_cos[kPart ? 1 : kMaxTiles * kTile];   // the nearest of the groups before
+    __shared__ int run_c[kPart ? 1 : kMaxTiles * kTile];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int64_t all = (N + kTile - 1) / kTile, tile0 = (int64_t)blockIdx.x * tiles;
+    const int count = (int)min((int64_t)tiles, all - tile0), parts = (W + kBlocks - 1) / kBlocks;
+    const int g0 = blockIdx.y * groups, g1 = min(g0 + groups, (C + kTile - 1) / kTile);
+
+    v4u code[kSteps];
+    uint32_t scale[kSteps / 4];   // a byte a step, less `top` (modulo 2^32, all four together): 127 for the row's largest
+    int top = 0, need = 1;        // the row's largest scale less 127; passes that the wave needs
+    constexpr int kAhead = kSteps <= 20 ? 1 : 0;   // words of the next sample asked for before this one's products, or after them
+    uint32_t word[1 + kAhead][kSteps];
+
+    // Words of sample tile i in part z of the row.  (Past the row's end, where the codes are zero, any word does.)
+    auto ask = [&](int i, int z, uint32_t(&to)[kSteps]) {
+        const int64_t n = min((tile0 + i) * kTile + col, N - 1);
+        const int w0 = z * kBlocks + wave * 2 * kSteps, first = w0 + half * kSteps;
+        if (w0 + 2 * kSteps <= W) {
+            __builtin_memcpy(to, hv + n * W + first, sizeof(to));
+        } else {
+            const uint32_t *const at = hv + anew(n * W);
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) {
+                to[t] = at[min(first + t, W - 1)];
+                if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (not all addresses at once)
+            }
+        }
+    };
+    // This wave's codes of a group of classes in part z.
+    auto hold = [&](int group, int z) {
+        const int c = group * kTile + col, first = z * kBlocks + (wave * 2 + half) * kSteps;
+        int s[kSteps], most = -1, least = 256;
+        bool none = false;
+        const int64_t from = anew((int64_t)min(c, C - 1) * W);
+        const v4u *const here = reinterpret_cast<const v4u *>(codes) + from;
+        if (first - half * kSteps + 2 * kSteps <= W) {
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) code[t] = here[first + t];
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) s[t] = scales[from + first + t];
+        } else {
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) {
+                code[t] = here[min(first + t, W - 1)];
+                s[t] = scales[from + min(first + t, W - 1)];
+                if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t) {
+            if (c >= C || first + t >= W) code[t] = v4u{0, 0, 0, 0}, s[t] = kQuantZero;
+            if (s[t] == kQuantNone) code[t] = v4u{0, 0, 0, 0}, none = true;
+            if (((code[t][0] | code[t][1] | code[t][2] | code[t][3]) & 0x77777777u) == 0) s[t] = -1;   // counts for nothing
+            most = max(most, s[t]);
+            least = min(least, s[t] < 0 ? 256 : s[t]);
+        }
+        most = max(most, __shfl_xor(most, 32, kWave));
+        least = min(least, __shfl_xor(least, 32, kWave));
+        none |= (bool)__shfl_xor((int)none, 32, kWave);
+        need = most < 0 ? 1 : (most - least) / (kRange + 1) + 1;
+        for (int off = 1; off < 32; off <<= 1) need = max(need, __shfl_xor(need, off, kWave));
+        need = __builtin_amdgcn_readfirstlane(need);
+        top = most - kQuantZero;
+#pragma unroll
+        for (int t = 0; t < kSteps; t += 4) {   // (blocks of zeros as the largest)
+            scale[t / 4] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) scale[t / 4] |= (uint32_t)(s[t + j] < 0 ? max(most, 0) : s[t + j]) << 8 * j;
+            scale[t / 4] -= 0x01010101u * (uint32_t)top;
+        }
+        __syncthreads();   // what is written here has been read
+        if (lane == 0) passes_of[wave] = need;
+        if (half == 0) units[wave][col] = none ? scale_value(kQuantNone) : most < 0 ? 1.0 : scale_value(most);
+    };
+
+    int turn = 0;
+    ask(0, 0, word[0]);
+    for (int g = g0; g < g1; ++g) {
+        const int n_of = tid & 31, c_of = g * kTile + (tid >> 5) * 2;   // this thread's sample and classes of a tile
+        for (int i = 0; i < count; ++i) {
+            double total[2] = {0.0, 0.0};
+            for (int z = 0; z < parts; ++z) {
+                if (parts > 1 || i == 0) hold(g, z);
+                const bool last = z + 1 == parts;
+                if (kAhead) ask(last ? (i + 1 < count ? i + 1 : 0) : i, last ? 0 : z + 1, word[kAhead]);
+                double down = 1.0;
+                for (int p = 0, passes = 1; p < passes; ++p) {
+                    v16f acc = {};
+#pragma unroll
+                    for (int t = 0; t < kSteps; ++t) word[0][t] = anew(word[0][t]);   // (or all signs would be made before the loop)
+                    top = anew(top);
+                    if (__builtin_expect(need == 1 && p == 0, 1)) {
+#pragma unroll
+                        for (int t = 0; t < kSteps; t += 4) {
+                            acc = mfma<0>(code[t], signs_of(word[0][t]), acc, scale[t / 4]);
+                            acc = mfma<1>(code[t + 1], signs_of(word[0][t + 1]), acc, scale[t / 4]);
+                            acc = mfma<2>(code[t + 2], signs_of(word[0][t + 2]), acc, scale[t / 4]);
+                            acc = mfma<3>(code[t + 3], signs_of(word[0][t + 3]), acc, scale[t / 4]);
+                            __builtin_amdgcn_sched_barrier(0);   // (not all signs at once: their registers)
+                        }
+                    } else {   // the blocks whose scale is one of this pass's: from 2^-(kRange + 1) p of the largest on downwards
+#pragma unroll
+                        for (int t = 0; t < kSteps; ++t) {
+                            const int of = (int)((scale[t / 4] + 0x01010101u * (uint32_t)top) >> 8 * (t & 3) & 255) - top + (kRange + 1) * p;
+                            const uint32_t mine = of <= kQuantZero && of >= kQuantZero - kRange ? ~0u : 0u;
+                            acc = mfma<0>(code[t] & mine, signs_of(word[0][t]), acc, (uint32_t)of & mine);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                    float(*const to)[kTile + 1] = sums[turn][wave];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) to[8 * (j / 4) + 4 * half + j % 4][col] = acc[j];
+                    __syncthreads();
+#pragma unroll 4
+                    for (int w = 0; w < kWaves; ++w) {
+                        passes = max(passes, passes_of[w]);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            total[j] = fma((double)sums[turn][w][(tid >> 5) * 2 + j][n_of], units[w][(tid >> 5) * 2 + j] * down, total[j]);
+                    }
+                    turn ^= 1;
+                    down *= 1.0 / (2 << kRange);
+                }
+                if constexpr (kAhead) {
+#pragma unroll
+                    for (int t = 0; t < kSteps; ++t) word[0][t] = word[kAhead][t];
+                } else {
+                    ask(last ? (i + 1 < count ? i + 1 : 0) : i, last ? 0 : z + 1, word[0]);
+                }
+            }
+            const int64_t n = (tile0 + i) * kTile + n_of;
+            if constexpr (kPart) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (n < N && c_of + j < C) part[n * C + c_of + j] = total[j];
+            } else {
+                Best best = {-__builtin_inf(), kNoClass};
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (c_of + j < C) {
+                        const double of = norm[c_of + j], cs = of == 0.0 ? 0.0 : total[j] / (sqrt(of) * root_d);
+                        if (cos_out && n < N) cos_out[n * C + c_of + j] = (float)cs;
+                        best = better(best, Best{cs, c_of + j});
+                    }
+                best = better(best, Best{__shfl_xor(best.cos, 32, kWave), __shfl_xor(best.c, 32, kWave)});
+                if (half == 0) near_cos[wave][col] = best.cos, near_c[wave][col] = best.c;
+                __syncthreads();
+                if (tid < kTile) {
+                    if (g > g0) best = better(Best{run_cos[i * kTile + col], run_c[i * kTile + col]}, best);
+#pragma unroll
+                    for (int w = 1; w < kWaves; ++w) best = better(best, Best{near_cos[w][col], near_c[w][col]});
+                    if (g + 1 < g1) {
+                        run_cos[i * kTile + col] = best.cos, run_c[i * kTile + col] = best.c;
+                    } else if (n < N) {
+                        if (pred_out) {
+                            pred_out[n] = best.c == kNoClass ? 0 : best.c;
+                        } else {
+                            best_cos[(int64_t)blockIdx.y * N + n] = best.cos;
+                            best_c[(int64_t)blockIdx.y * N + n] = best.c;
+                        }
+                    }
+                }
+            }
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void nearest_kernel(const double *__restrict__ best_cos, const int *__restrict__ best_c, int64_t N, int splits,
+                                                      int32_t *__restrict__ pred) {
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= N) return;
+    Best best = {best_cos[n], best_c[n]};
+    for (int k = 1; k < splits; ++k) best = better(best, Best{best_cos[k * N + n], best_c[k * N + n]});
+    pred[n] = best.c == kNoClass ? 0 : best.c;
+}
+
+// Steps of a wave: as many as a row needs, up to 32 (the registers) at a time.
+int steps_of(int W) {
+    const int parts = (W + kWaves * 64 - 1) / (kWaves * 64), per = (W + parts - 1) / parts;
+    return ((per + kWaves * 2 - 1) / (kWaves * 2) + 3) / 4 * 4;
+}
+
+template <bool kPart>
+void launch(hdc_ctx_impl *c, dim3 grid, hipStream_t s, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
+            int tiles, int groups, double *part, float *cos_out, int32_t *pred, double *best_cos, int *best_c) {
+#define HDC_SEARCH(STEPS)                                                                                                                                \
+    hipLaunchKernelGGL((search_quantized_kernel<STEPS, kPart>), grid, dim3(kThreads), 0, s, hv, N, c->W, c->p.C, codes, scales, norm, sqrt((double)c->p.D), \
+                       tiles, groups, part, cos_out, pred, best_cos, best_c)
+    switch (steps_of(c->W)) {
+        case 4: HDC_SEARCH(4); break;
+        case 8: HDC_SEARCH(8); break;
+        case 12: HDC_SEARCH(12); break;
+        case 16: HDC_SEARCH(16); break;
+        case 20: HDC_SEARCH(20); break;
+        case 24: HDC_SEARCH(24); break;
+        case 28: HDC_SEARCH(28); break;
+        default: HDC_SEARCH(32); break;
+    }
+#undef HDC_SEARCH
+}
+
+}  // namespace
+
+// Entries of the scratch where the nearest classes of splits meet: a launch has splits only while its tiles leave compute units idle.
+int64_t search_quantized_entries(const hdc_ctx_impl *c) { return (int64_t)kTile * c->num_cus; }
+
+int launch_search_quantized(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
+                            float *cos_out, int32_t *pred, hipStream_t s) {
+    ProfScope prof(c, HDC_K_SEARCH_QUANTIZED, s);
+    const int groups = (c->p.C + kTile - 1) / kTile;
+    const int64_t tiles = (N + kTile - 1) / kTile, cus = c->num_cus;
+    // One block a compute unit.  One group of classes: as many tiles as that gives a block; more groups: the block walks over its tiles
+    // for each, and where there are fewer tiles than compute units, the groups are split among blocks.
+    int64_t per = std::max<int64_t>(1, (tiles + cus - 1) / cus);
+    if (groups > 1) per = std::min<int64_t>(per, kMaxTiles);
+    const int splits_most = (int)std::max<int64_t>(1, std::min<int64_t>(groups, cus / tiles));
+    const int of_split = (groups + splits_most - 1) / splits_most, splits = (groups + of_split - 1) / of_split;
+    const int64_t blocks = (tiles + per - 1) / per, most = 1 << 22;   // blocks a launch
+    for (int64_t b = 0; b < blocks; b += most) {
+        const int64_t n0 = b * per * kTile, n = std::min(N - n0, most * per * kTile);
+        launch<false>(c, dim3((unsigned)std::min(most, blocks - b), (unsigned)splits), s, hv + n0 * c->W, n, codes, scales, norm, (int)per, of_split, nullptr,
+                      cos_out ? cos_out + n0 * c->p.C : nullptr, splits > 1 ? nullptr : pred + n0, c->qs_cos_d, c->qs_class_d);
+    }
+    if (splits > 1)
+        hipLaunchKernelGGL(nearest_kernel, dim3((unsigned)((N + 255) / 256)), dim3(256), 0, s, c->qs_cos_d, c->qs_class_d, N, splits, pred);
+    HDC_HIP(hipGetLastError());
+    return HDC_OK;
+}
+
+int launch_quantized_dots(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const uint32_t *codes, const uint8_t *scales, double *part, int *slices,
+                          hipStream_t s) {
+    ProfScope prof(c, HDC_K_ONLINE_FWD, s);
+    *slices = 1;
+    const int64_t tiles = (nb + kTile - 1) / kTile, groups = (c->p.C + kTile - 1) / kTile;
+    const int64_t per = std::max<int64_t>(1, (tiles * groups + c->num_cus - 1) / c->num_cus);
+    launch<true>(c, dim3((unsigned)((tiles + per - 1) / per), (unsigned)groups), s, hv, nb, codes, scales, nullptr, (int)per, 1, part, nullptr, nullptr, nullptr,
+                 nullptr);
+    HDC_HIP(hipGetLastError());
+    return HDC_OK;
+}
+
+}  // namespace hdc

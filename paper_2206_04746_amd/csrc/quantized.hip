@@ -13,65 +13,118 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
-// A block of threads a row, a thread a block of 32 dimensions at a time.
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const float *__restrict__ rows, int64_t N, int D, int W, uint32_t *__restrict__ codes,
-                                                            uint8_t *__restrict__ scales, double *__restrict__ norm, double *__restrict__ part, int G) {
-    __shared__ double sums[4];
-    const int tid = threadIdx.x;
-    for (int64_t n = blockIdx.x; n < N; n += gridDim.x) {
+// Lane exchanges within a row of 16: with the neighbour, with the neighbour's neighbour, and among eight lanes from the other end.
+template <int kSel>
+__device__ __forceinline__ uint32_t lanes(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kSel, 0xF, 0xF, true);
+}
+constexpr int kNext = 0xB1, kNextPair = 0x4E, kMirrorEight = 0x141;
+
+// Squares of the magnitudes in halves, by code: 0 1 4 9 16 36 64 144.
+__device__ __forceinline__ int squares(uint32_t four) {
+    return (int)__builtin_amdgcn_udot4(__builtin_amdgcn_perm(0x90402410u, 0x09040100u, four & 0x07070707u), 0x01010101u, 0u, false);
+}
+
+// Eight lanes a block of 32 dimensions, four adjacent ones a lane; a wave eight blocks at a time, twice.  Four elements become four codes
+// in the bytes of a register (v_cvt_scalef32_pk_fp4_f32: nearest, ties to even, beyond 6 it is 6), and the eight lanes' registers the
+// block's four words by two byte permutes: so rows are read in order and words written in order.  Bound by memory.
+// A block of threads a row (or, with norms by groups of 64 dimensions, `chunks` blocks); norm: the row's, or part: [row][group].
+__global__ __launch_bounds__(1024) void quantize_rows_kernel(const float *__restrict__ rows, int64_t N, int D, int W, uint32_t *__restrict__ codes,
+                                                             uint8_t *__restrict__ scales, double *__restrict__ norm, double *__restrict__ part, int G) {
+    __shared__ double sums[16];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, waves = blockDim.x >> 6;
+    const int j = lane & 7, pair = j >> 1;
+    // A lane of pair q takes byte r of its own register and of pair q ^ 1's for its word's half, then halves from pair q ^ 2.
+    const uint32_t pick = pair & 1 ? 0x03070105u : 0x06020400u, half = pair & 2 ? 0x03020706u : 0x05040100u;
+    for (int64_t n = blockIdx.y; n < N; n += gridDim.y) {
+        const float *const row = rows + n * D;
         double mine = 0.0;
-        for (int w = tid; w < W; w += 256) {
-            const float *x = rows + n * D + (int64_t)w * 32;
-            const int count = min(32, D - w * 32);
-            uint32_t most = 0;   // of the magnitudes' bits, which are ordered like the numbers
-            for (int i = 0; i < count; ++i) most = max(most, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-            int s = kQuantNone;
-            uint32_t word[4] = {0, 0, 0, 0};
-            if (most < 0x7F800000u) {
-                s = max((int)(most >> 23) - 2, 0);   // floor(log2) less 2; what is below 2^-126 has 2^-127
-                const double unit = scale_value(254 - s);
-                for (int i = 0; i < count; ++i) {
-                    const double v = fabs((double)x[i]) * unit;
-                    uint32_t code = (v > 0.25) + (v >= 0.75) + (v > 1.25) + (v >= 1.75) + (v > 2.5) + (v >= 3.5) + (v > 5.0);
-                    code |= __float_as_uint(x[i]) >> 31 << 3;
-                    word[i & 3] |= code << (i & ~3);
+        for (int w0 = (blockIdx.x * waves + wave) * 16; w0 < W; w0 += gridDim.x * waves * 16) {   // uniform
+            uint32_t x[2][4], word[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int d = (w0 + 8 * k) * 32 + lane * 4;
+                if (d + 4 <= D) {
+                    __builtin_memcpy(x[k], row + d, 16);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[k][r] = d + r < D ? __float_as_uint(row[d + r]) : 0u;
                 }
             }
-            int q = 0;
-            for (int i = 0; i < 32; ++i) {
-                const int h = code_halves(word[i & 3] >> (i & ~3));
-                q += h * h;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int w = w0 + 8 * k + (lane >> 3);
+                uint32_t most = 0;   // of the magnitudes' bits, which are ordered like the numbers
+#pragma unroll
+                for (int r = 0; r < 4; ++r) most = max(most, x[k][r] & 0x7FFFFFFFu);
+                most = max(most, lanes<kNext>(most));
+                most = max(most, lanes<kNextPair>(most));
+                most = max(most, lanes<kMirrorEight>(most));
+                const bool none = most >= 0x7F800000u;
+                const int s = max((int)(most >> 23) - 2, 0);   // floor(log2) less 2; what is below 2^-126 has 2^-127
+                const float unit = __uint_as_float(s ? (uint32_t)s << 23 : 0x00400000u);
+                uint32_t four = 0;
+                if (!none) {
+                    four = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(four, __uint_as_float(x[k][0]), 0.0f, unit, 0);
+                    four = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(four, __uint_as_float(x[k][1]), 0.0f, unit, 1);
+                    four = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(four, __uint_as_float(x[k][2]), 0.0f, unit, 2);
+                    four = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(four, __uint_as_float(x[k][3]), 0.0f, unit, 3);
+                }
+                // a quarter of the square of the scale
+                const double square = none ? scale_value(kQuantNone) : __longlong_as_double((long long)(2 * s + 1023 - 2 * kQuantZero - 2) << 52);
+                mine = fma((double)squares(four), square, mine);
+                if (part) {   // sixteen lanes a group
+                    for (int off = 1; off < 16; off <<= 1) mine += __shfl_xor(mine, off, kWave);
+                    if ((lane & 15) == 0 && w < W) part[n * G + w / 2] = mine;
+                    mine = 0.0;
+                }
+                four <<= 4 * (j & 1);
+                four |= lanes<kNext>(four);
+                const uint32_t two = __builtin_amdgcn_perm(lanes<kNextPair>(four), four, pick);
+                word[k] = __builtin_amdgcn_perm(lanes<kNextPair>(lanes<kMirrorEight>(two)), two, half);
+                if (j == 0 && w < W) scales[n * W + w] = (uint8_t)(none ? kQuantNone : s);
             }
-            mine += (double)q * (0.25 * scale_value(s)) * scale_value(s);
-            for (int i = 0; i < 4; ++i) codes[((int64_t)n * W + w) * 4 + i] = word[i];
-            scales[(int64_t)n * W + w] = (uint8_t)s;
-            if (part) {
-                const double other = __shfl_xor(mine, 1, kWave);
-                if ((w & 1) == 0) part[n * G + w / 2] = w + 1 < W ? mine + other : mine;
-                mine = 0.0;
-            }
+            const int w = w0 + 8 * (j & 1) + (lane >> 3);
+            if (w < W) codes[(n * W + w) * 4 + pair] = word[j & 1];
         }
         if (norm) {
             const double sum = wave_sum(mine);
-            if ((tid & 63) == 0) sums[tid >> 6] = sum;
+            if (lane == 0) sums[wave] = sum;
             __syncthreads();
-            if (tid == 0) norm[n] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            if (tid == 0) {
+                double all = sums[0];
+                for (int i = 1; i < waves; ++i) all += sums[i];
+                norm[n] = all;
+            }
             __syncthreads();
         }
     }
 }
 
-// A thread four adjacent dimensions.
+// Eight lanes a block, four adjacent dimensions a lane: nibble j of each of the block's words.
 __global__ __launch_bounds__(256) void dequantize_rows_kernel(const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t N, int D,
                                                               int W, float *__restrict__ rows) {
-    for (int64_t n = blockIdx.x; n < N; n += gridDim.x)
-        for (int d = threadIdx.x * 4; d < D; d += 1024) {
-            const int w = d / 32, j = d % 32;
-            const double unit = 0.5 * scale_value(scales[n * W + w]);
-            for (int r = 0; r < 4 && d + r < D; ++r) {
-                const uint32_t code = codes[(n * W + w) * 4 + r] >> j & 15;
-                const float v = (float)(code_halves(code) * unit);
-                rows[n * D + d + r] = code & 8 ? -v : v;
+    const int tid = threadIdx.x, shift = 4 * (tid & 7);
+    for (int64_t n = blockIdx.y; n < N; n += gridDim.y)
+        for (int w = blockIdx.x * 32 + (tid >> 3); w < W; w += gridDim.x * 32) {
+            const int d = w * 32 + shift;
+            const v4u word = *reinterpret_cast<const v4u *>(codes + (n * W + w) * 4);
+            const int s = scales[n * W + w];
+            uint32_t four = 0, x[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) four |= (word[r] >> shift & 15) << 8 * r;
+            const uint32_t halves = __builtin_amdgcn_perm(0x0C080604u, 0x03020100u, four & 0x07070707u);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t v = __float_as_uint(ldexpf((float)(halves >> 8 * r & 255), s - kQuantZero - 1));
+                x[r] = s == kQuantNone ? 0x7FC00000u : v | (four >> 8 * r & 8) << 28;
+            }
+            if (d + 4 <= D) {
+                __builtin_memcpy(rows + n * D + d, x, 16);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (d + r < D) rows[n * D + d + r] = __uint_as_float(x[r]);
             }
         }
 }
@@ -99,16 +152,23 @@ __global__ __launch_bounds__(256) void product_quantized_kernel(const uint32_t *
 
 }  // namespace
 
+// Rows beyond a launch's 65535 are taken by the same blocks.
 int launch_quantize(hdc_ctx_impl *c, const float *rows, int64_t N, uint32_t *codes, uint8_t *scales, double *norm, double *part, hipStream_t s) {
     ProfScope prof(c, HDC_K_QUANTIZE_ROWS, s);
-    hipLaunchKernelGGL(quantize_rows_kernel, dim3((unsigned)std::min<int64_t>(N, 1 << 20)), dim3(256), 0, s, rows, N, c->p.D, c->W, codes, scales, norm, part,
-                       (c->p.D + kWave - 1) / kWave);
+    // A wave to 512 dimensions, a block of up to sixteen waves to a row: four where there are rows enough for every compute unit's.
+    // Without norms to be summed over the row, several blocks where there are few rows.
+    const int steps = (c->W + 15) / 16, waves = std::min(steps, N >= 8 * (int64_t)c->num_cus ? 4 : norm ? 16 : 4);
+    const int chunks = norm ? 1 : (int)std::min<int64_t>((steps + waves - 1) / waves, std::max<int64_t>(1, 8 * (int64_t)c->num_cus / N));
+    hipLaunchKernelGGL(quantize_rows_kernel, dim3((unsigned)chunks, (unsigned)std::min<int64_t>(N, 65535)), dim3((unsigned)waves * kWave), 0, s, rows, N,
+                       c->p.D, c->W, codes, scales, norm, part, (c->p.D + kWave - 1) / kWave);
     HDC_HIP(hipGetLastError());
     return HDC_OK;
 }
 
 int launch_dequantize(hdc_ctx_impl *c, const uint32_t *codes, const uint8_t *scales, int64_t N, float *rows, hipStream_t s) {
-    hipLaunchKernelGGL(dequantize_rows_kernel, dim3((unsigned)std::min<int64_t>(N, 1 << 20)), dim3(256), 0, s, codes, scales, N, c->p.D, c->W, rows);
+    const int64_t chunks = (c->W + 31) / 32;
+    const dim3 grid((unsigned)std::min(chunks, std::max<int64_t>(1, 64 * (int64_t)c->num_cus / N)), (unsigned)std::min<int64_t>(N, 65535));
+    hipLaunchKernelGGL(dequantize_rows_kernel, grid, dim3(256), 0, s, codes, scales, N, c->p.D, c->W, rows);
     HDC_HIP(hipGetLastError());
     return HDC_OK;
 }

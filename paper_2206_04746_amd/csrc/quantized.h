@@ -18,6 +18,14 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ int code_halves(uint32_t code) { return (int)(0x0C08060403020100ull >> 8 * (code & 7) & 255); }
 __device__ __forceinline__ int code_signed_halves(uint32_t code) { return code & 8 ? -code_halves(code) : code_halves(code); }
 
+// The same number, of which the compiler does not know that it is: what is computed from it is computed here, and not kept in registers
+// from before a loop.
+template <typename T>
+__device__ __forceinline__ T anew(T v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // 2^(s - 127) in 64 bits; a quiet NaN for a block that is no number.
 __device__ __forceinline__ double scale_value(int s) {
     return s == kQuantNone ? __longlong_as_double(0x7FF8000000000000ll) : __longlong_as_double((long long)(s + 896) << 52);

@@ -1,4 +1,4 @@
-// Class rows in 4-bit floats: quantisation and its way back, and products (arXiv 2206.04746, Sec. III, with rows between
+// Class rows in 4-bit floats: quantisation and its way back (arXiv 2206.04746, Sec. III, with rows between
 // the bits of hdc_binarize_online and the 32-bit floats of hdc_search_cosine).
 #include <algorithm>
 
@@ -129,27 +129,6 @@ __global__ __launch_bounds__(256) void dequantize_rows_kernel(const uint32_t *__
         }
 }
 
-// A wave a product of two rows.
-__global__ __launch_bounds__(256) void product_quantized_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
-                                                                const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb, int64_t N, int W,
-                                                                float *__restrict__ out) {
-    const int lane = threadIdx.x & 63;
-    for (int64_t m = blockIdx.y; m < M; m += gridDim.y)
-        for (int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); n < N; n += (int64_t)gridDim.x * 4) {
-            double dot = 0.0;
-            for (int w = lane; w < W; w += kWave) {
-                int sum = 0;
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t x = a[(m * W + w) * 4 + i], y = b[(n * W + w) * 4 + i];
-                    for (int j = 0; j < 32; j += 4) sum += code_signed_halves(x >> j) * code_signed_halves(y >> j);
-                }
-                dot += sum * (0.5 * scale_value(sa[m * W + w])) * (0.5 * scale_value(sb[n * W + w]));
-            }
-            dot = wave_sum(dot);
-            if (lane == 0) out[m * N + n] = (float)dot;
-        }
-}
-
 }  // namespace
 
 // Rows beyond a launch's 65535 are taken by the same blocks.
@@ -169,15 +148,6 @@ int launch_dequantize(hdc_ctx_impl *c, const uint32_t *codes, const uint8_t *sca
     const int64_t chunks = (c->W + 31) / 32;
     const dim3 grid((unsigned)std::min(chunks, std::max<int64_t>(1, 64 * (int64_t)c->num_cus / N)), (unsigned)std::min<int64_t>(N, 65535));
     hipLaunchKernelGGL(dequantize_rows_kernel, grid, dim3(256), 0, s, codes, scales, N, c->p.D, c->W, rows);
-    HDC_HIP(hipGetLastError());
-    return HDC_OK;
-}
-
-int launch_product_quantized(hdc_ctx_impl *c, const uint32_t *a, const uint8_t *sa, int64_t M, const uint32_t *b, const uint8_t *sb, int64_t N, float *out,
-                             hipStream_t s) {
-    ProfScope prof(c, HDC_K_PRODUCT_QUANTIZED, s);
-    const dim3 grid((unsigned)std::min<int64_t>((N + 3) / 4, 1 << 20), (unsigned)std::min<int64_t>(M, 65535));
-    hipLaunchKernelGGL(product_quantized_kernel, grid, dim3(256), 0, s, a, sa, M, b, sb, N, c->W, out);
     HDC_HIP(hipGetLastError());
     return HDC_OK;
 }

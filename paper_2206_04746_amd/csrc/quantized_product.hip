@@ -1,0 +1,255 @@
+// Products of rows of 4-bit floats with one another: out[m][n] = <a[m], b[n]>, on v_mfma_scale_f32_32x32x64_f8f6f4, which takes the
+// codes and the scales as they are stored and sums in fp32.
+//
+// Many rows: tiles of a's rows by b's rows through LDS, 256 dimensions at a time (128 bytes a row, loaded straight into LDS).  A wave takes
+// its operands of such a step into registers at once, so that the next step's can be loaded over them while it multiplies: a block needs
+// one buffer, and two blocks share a compute unit, one loading while the other multiplies.
+// Few rows: a block takes 32 by 32 rows, its waves a part of the dimensions each, without LDS but for the sum over the waves.
+#include <algorithm>
+#include <type_traits>
+
+#include "quantized.h"
+
+namespace hdc {
+
+namespace {
+
+constexpr int kTile = 32;   // rows of either side to a matrix instruction
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+template <int B>
+__device__ __forceinline__ v16f mfma(v4u a, v4u b, v16f c, uint32_t sa, uint32_t sb) {
+    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, B, (int)sa, B, (int)sb);
+}
+
+// Bytes [at, at + kBytes) of a row's scales as words; past the row's end those of 1.
+template <int kBytes>
+__device__ __forceinline__ void scale_bytes(const uint8_t *row, int at, int W, uint32_t (&out)[kBytes / 4]) {
+    if (at + kBytes <= W) {
+        __builtin_memcpy(out, row + at, kBytes);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kBytes / 4; ++i) {
+            uint32_t s[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[k] = row[min(at + 4 * i + k, W - 1)];
+            out[i] = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) out[i] |= (at + 4 * i + k < W ? s[k] : kQuantZero) << 8 * k;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
+// ---- few rows: 32 of a by 32 of b a block; the halves of a wave's lanes take steps of 32 dimensions from places of their own
+constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave;
+
+__global__ __launch_bounds__(kFewThreads) void product_few_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
+                                                                  const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb, int64_t N, int W,
+                                                                  int steps, float *__restrict__ out) {
+    __shared__ float sums[kFewWaves][kTile][kTile + 1];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int64_t m0 = (int64_t)blockIdx.y * kTile, n0 = (int64_t)blockIdx.x * kTile;
+    const int64_t ra = min(m0 + col, M - 1) * W, rb = min(n0 + col, N - 1) * W;
+    const v4u *const ca = reinterpret_cast<const v4u *>(a) + ra, *const cb = reinterpret_cast<const v4u *>(b) + rb;
+    const int first = (wave * 2 + half) * steps;   // steps: a multiple of 4
+    v16f acc = {};
+    for (int t = 0; t < steps; t += 4) {
+        v4u x[4], y[4];
+        uint32_t sx[1], sy[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int w = first + t + i, in = min(w, W - 1);
+            x[i] = ca[in], y[i] = cb[in];
+            if (w >= W) x[i] = v4u{0, 0, 0, 0}, y[i] = v4u{0, 0, 0, 0};
+        }
+        scale_bytes<4>(sa + ra, first + t, W, sx);
+        scale_bytes<4>(sb + rb, first + t, W, sy);
+        acc = mfma<0>(x[0], y[0], acc, sx[0], sy[0]);
+        acc = mfma<1>(x[1], y[1], acc, sx[0], sy[0]);
+        acc = mfma<2>(x[2], y[2], acc, sx[0], sy[0]);
+        acc = mfma<3>(x[3], y[3], acc, sx[0], sy[0]);
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sums[wave][8 * (j / 4) + 4 * half + j % 4][col] = acc[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int r = (tid >> 5) + 16 * j;
+        double sum = 0.0;   // of eight fp32 sums, rounded once
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) sum += (double)sums[w][r][col];
+        if (m0 + r < M && n0 + col < N) out[(m0 + r) * N + n0 + col] = (float)sum;
+    }
+}
+
+// ---- many rows: a tile of 64 kA rows of a by 64 kB of b a block of two by two waves
+constexpr int kThreads = 256, kStep = 8, kUnit = 16;   // blocks of 32 dimensions a step, bytes of one
+constexpr int kScaleSteps = 4;                         // steps whose scales are in LDS together
+
+// Blocks of 32 dimensions, `at` bytes into the rows, of kOf rows into LDS, a wave eight rows at a time.
+template <int kOf>
+__device__ __forceinline__ void load_rows(const uint32_t *first, int rows, uint32_t pitch, uint32_t at, int wave, int lane, uint32_t *to) {
+    const auto from = __builtin_amdgcn_make_buffer_rsrc((void *)first, 0, (int)(rows * pitch), 0x00020000);
+    const int l = anew(lane) >> 3;   // (no address is kept through the products)
+    if (rows == kOf) {
+        const uint32_t mine = (uint32_t)l * pitch + at;
+#pragma unroll
+        for (int i = 0; i < kOf / 32; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)(to + (i * 32 + wave * 8) * kStep * 4), kUnit, (int)mine,
+                                                     (int)((i * 32 + wave * 8) * pitch), 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kOf / 32; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)(to + (i * 32 + wave * 8) * kStep * 4), kUnit,
+                                                     (int)((uint32_t)min(i * 32 + wave * 8 + l, rows - 1) * pitch + at), 0, 0, 0);
+    }
+}
+
+template <int kA, int kB>
+__global__ __launch_bounds__(kThreads, 2) void product_tiles_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
+                                                                    const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb, int64_t N, int W,
+                                                                    int tiles_m, int tiles_n, float *__restrict__ out) {
+    constexpr int kRowsA = 64 * kA, kRowsB = 64 * kB, kRows = kRowsA + kRowsB;
+    constexpr int kPieces = kRows * 2 * kScaleSteps * kStep / 32 / kThreads;   // 16 bytes of scales
+    // Codes: block k of a row's eight is at place k ^ (row % 8) of the row, so that eight rows' blocks lie in different banks.
+    __shared__ __align__(16) uint32_t unit[kRows * kStep * 4];
+    __shared__ uint32_t scale[2][kScaleSteps * kStep / 4][kRows];   // of these steps and the next ones
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+
+    // Blocks of consecutive numbers go to the eight dies in turn: a die takes tiles that lie together, eight rows of tiles wide.
+    int tm, tn;
+    {
+        const int all = tiles_m * tiles_n, die = blockIdx.x % 8, per = all / 8, more = all % 8;
+        const int at = die * per + min(die, more) + blockIdx.x / 8;
+        const int band = at / (8 * tiles_n), high = min(8, tiles_m - band * 8), in = at - band * 8 * tiles_n;
+        tm = __builtin_amdgcn_readfirstlane(band * 8 + in % high), tn = __builtin_amdgcn_readfirstlane(in / high);
+    }
+    const int64_t m0 = (int64_t)tm * kRowsA, n0 = (int64_t)tn * kRowsB;
+    const int rows_a = (int)min((int64_t)kRowsA, M - m0), rows_b = (int)min((int64_t)kRowsB, N - n0);
+    const uint32_t pitch = (uint32_t)W * kUnit;
+    const int steps = (W + kStep - 1) / kStep;
+
+    // A wave's load fills eight rows of 128 bytes.  Rows and blocks past the end are taken from the last ones.
+    auto load = [&](int step) {
+        const uint32_t at = (uint32_t)min(step * kStep + ((lane & 7) ^ (lane >> 3)), W - 1) * kUnit;
+        load_rows<kRowsA>(a + m0 * W * 4, rows_a, pitch, at, wave, lane, unit);
+        load_rows<kRowsB>(b + n0 * W * 4, rows_b, pitch, at, wave, lane, unit + kRowsA * kStep * 4);
+    };
+    uint32_t piece[kPieces][4];
+    auto ask_scales = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int p = anew(tid) + i * kThreads, r = p % kRows, at = step * kStep + p / kRows * 16;
+            const uint8_t *const row = r < kRowsA ? sa + (m0 + min(r, rows_a - 1)) * W : sb + (n0 + min(r - kRowsA, rows_b - 1)) * W;
+            scale_bytes<16>(row, at, W, piece[i]);
+        }
+    };
+    auto put_scales = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int p = anew(tid) + i * kThreads;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) scale[step / kScaleSteps % 2][p / kRows * 4 + j][p % kRows] = piece[i][j];
+        }
+    };
+
+    const int wm = (wave >> 1) * 32 * kA, wn = kRowsA + (wave & 1) * 32 * kB;   // this wave's rows
+    v16f acc[kA][kB] = {};
+    v4u x[kA][4], y[kB][4];
+    uint32_t sx[kA], sy[kB];
+    auto take = [&](int t) {
+        const uint32_t *const from = unit + (col * kStep + ((4 * half + t) ^ (col & 7))) * 4;
+#pragma unroll
+        for (int i = 0; i < kA; ++i) x[i][t] = *reinterpret_cast<const v4u *>(from + (wm + i * 32) * kStep * 4);
+#pragma unroll
+        for (int i = 0; i < kB; ++i) y[i][t] = *reinterpret_cast<const v4u *>(from + (wn + i * 32) * kStep * 4);
+    };
+    auto multiply = [&](auto t_of) {
+        constexpr int t = decltype(t_of)::value;
+#pragma unroll
+        for (int i = 0; i < kA; ++i)
+#pragma unroll
+            for (int j = 0; j < kB; ++j) acc[i][j] = mfma<t>(x[i][t], y[j][t], acc[i][j], sx[i], sy[j]);
+#pragma unroll
+        for (int i = 0; i < kA; ++i)   // here, and not past the next barrier: operands take the registers of those that have been multiplied
+#pragma unroll
+            for (int j = 0; j < kB; ++j) acc[i][j] = anew(acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    ask_scales(0);
+    load(0);
+    put_scales(0);
+    for (int k = 0; k < steps; ++k) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // what this wave loads into LDS; the barrier alone does not wait for it
+        __syncthreads();
+        if (k * kStep + kStep > W) {   // blocks past the row's end: zeros
+            for (int u = tid; u < kRows * kStep; u += kThreads)
+                if (k * kStep + ((u & 7) ^ (u >> 3 & 7)) >= W) *reinterpret_cast<v4u *>(unit + u * 4) = v4u{0, 0, 0, 0};
+            __syncthreads();
+        }
+        take(0);
+        const uint32_t(*const scales)[kRows] = &scale[k / kScaleSteps % 2][k % kScaleSteps * 2 + half];
+#pragma unroll
+        for (int i = 0; i < kA; ++i) sx[i] = scales[0][wm + i * 32 + col];
+#pragma unroll
+        for (int i = 0; i < kB; ++i) sy[i] = scales[0][wn + i * 32 + col];
+        take(1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(std::integral_constant<int, 0>{});
+        take(2);
+        take(3);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(std::integral_constant<int, 1>{});
+        __syncthreads();   // all operands are in registers
+        const bool more = k + 1 < steps, scales_too = more && (k + 1) % kScaleSteps == 0;
+        if (scales_too) ask_scales(k + 1);
+        if (more) load(k + 1);
+        multiply(std::integral_constant<int, 2>{});
+        multiply(std::integral_constant<int, 3>{});
+        if (scales_too) put_scales(k + 1);
+    }
+#pragma unroll
+    for (int i = 0; i < kA; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = wm + i * 32 + 8 * (r / 4) + 4 * half + r % 4;
+            if (row >= rows_a) continue;
+            float *const to = out + (m0 + row) * N + n0;
+#pragma unroll
+            for (int j = 0; j < kB; ++j) {
+                const int n = wn - kRowsA + j * 32 + col;
+                if (n < rows_b) to[n] = acc[i][j][r];
+            }
+        }
+}
+
+}  // namespace
+
+int launch_product_quantized(hdc_ctx_impl *c, const uint32_t *a, const uint8_t *sa, int64_t M, const uint32_t *b, const uint8_t *sb, int64_t N, float *out,
+                             hipStream_t s) {
+    ProfScope prof(c, HDC_K_PRODUCT_QUANTIZED, s);
+    const int W = c->W;
+    const int64_t few = ((M + 31) / 32) * ((N + 31) / 32), large = ((M + 255) / 256) * ((N + 127) / 128), small = ((M + 127) / 128) * ((N + 127) / 128);
+    if (few < 4 * (int64_t)c->num_cus || N < 64 || M < 64) {
+        const int steps = ((W + 2 * kFewWaves - 1) / (2 * kFewWaves) + 3) / 4 * 4;
+        for (int64_t m = 0; m < M; m += 32 * 65535) {
+            const int64_t rows = std::min<int64_t>(M - m, 32 * 65535);
+            hipLaunchKernelGGL(product_few_kernel, dim3((unsigned)((N + 31) / 32), (unsigned)((rows + 31) / 32)), dim3(kFewThreads), 0, s, a + m * W * 4,
+                               sa + m * W, rows, b, sb, N, W, steps, out + m * N);
+        }
+    } else if (large >= c->num_cus) {
+        hipLaunchKernelGGL((product_tiles_kernel<4, 2>), dim3((unsigned)large), dim3(kThreads), 0, s, a, sa, M, b, sb, N, W, (int)((M + 255) / 256),
+                           (int)((N + 127) / 128), out);
+    } else {
+        hipLaunchKernelGGL((product_tiles_kernel<2, 2>), dim3((unsigned)small), dim3(kThreads), 0, s, a, sa, M, b, sb, N, W, (int)((M + 127) / 128),
+                           (int)((N + 127) / 128), out);
+    }
+    HDC_HIP(hipGetLastError());
+    return HDC_OK;
+}
+
+}  // namespace hdc

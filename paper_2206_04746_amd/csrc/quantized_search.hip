@@ -46,14 +46,6 @@ __device__ __forceinline__ v4u signs_of(uint32_t word) {
     return out;
 }
 
-// The same number, of which the compiler does not know that it is: what is computed from it is computed here, and not kept in registers
-// from before a loop.
-template <typename T>
-__device__ __forceinline__ T anew(T v) {
-    asm volatile("" : "+v"(v));
-    return v;
-}
-
 struct Best {
     double cos;
     int c;

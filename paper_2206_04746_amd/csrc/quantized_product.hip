@@ -1,9 +1,8 @@
 // Products of rows of 4-bit floats with one another: out[m][n] = <a[m], b[n]>, on v_mfma_scale_f32_32x32x64_f8f6f4, which takes the
 // codes and the scales as they are stored and sums in fp32.
 //
-// Many rows: tiles of a's rows by b's rows through LDS, 256 dimensions at a time (128 bytes a row, loaded straight into LDS).  A wave takes
-// its operands of such a step into registers at once, so that the next step's can be loaded over them while it multiplies: a block needs
-// one buffer, and two blocks share a compute unit, one loading while the other multiplies.
+// Many rows: tiles of a's rows by b's rows through LDS, 256 dimensions at a time (128 bytes a row, loaded straight into LDS), the next step's
+// while a step's are multiplied; within a step a wave takes the operands of its next matrix instructions while it issues these.
 // Few rows: a block takes 32 by 32 rows, its waves a part of the dimensions each, without LDS but for the sum over the waves.
 #include <algorithm>
 #include <type_traits>
@@ -88,9 +87,10 @@ __global__ __launch_bounds__(kFewThreads) void product_few_kernel(const uint32_t
 
 // ---- many rows: a tile of 64 kA rows of a by 64 kB of b a block of two by two waves
 constexpr int kThreads = 256, kStep = 8, kUnit = 16;   // blocks of 32 dimensions a step, bytes of one
-constexpr int kScaleSteps = 4;                         // steps whose scales are in LDS together
+constexpr int kScaleSteps = 2;                         // steps whose scales are asked for together
 
-// Blocks of 32 dimensions, `at` bytes into the rows, of kOf rows into LDS, a wave eight rows at a time.
+// Blocks of 32 dimensions, `at` bytes into the rows, of kOf rows into LDS, a wave eight rows of 128 bytes at a time.  Rows past the last are
+// taken from it.
 template <int kOf>
 __device__ __forceinline__ void load_rows(const uint32_t *first, int rows, uint32_t pitch, uint32_t at, int wave, int lane, uint32_t *to) {
     const auto from = __builtin_amdgcn_make_buffer_rsrc((void *)first, 0, (int)(rows * pitch), 0x00020000);
@@ -109,15 +109,27 @@ __device__ __forceinline__ void load_rows(const uint32_t *first, int rows, uint3
     }
 }
 
+// The sums of a tile are computed here, and not past the next barrier: operands take the registers of those that have been multiplied.
+// (Sixteen tiles a wave are all of the accumulation registers.)
+template <bool kAccumulators>
+__device__ __forceinline__ v16f settled(v16f v) {
+    if constexpr (kAccumulators)
+        asm volatile("" : "+a"(v));
+    else
+        asm volatile("" : "+v"(v));
+    return v;
+}
+
 template <int kA, int kB>
-__global__ __launch_bounds__(kThreads, 2) void product_tiles_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
-                                                                    const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb, int64_t N, int W,
-                                                                    int tiles_m, int tiles_n, float *__restrict__ out) {
-    constexpr int kRowsA = 64 * kA, kRowsB = 64 * kB, kRows = kRowsA + kRowsB;
-    constexpr int kPieces = kRows * 2 * kScaleSteps * kStep / 32 / kThreads;   // 16 bytes of scales
-    // Codes: block k of a row's eight is at place k ^ (row % 8) of the row, so that eight rows' blocks lie in different banks.
-    __shared__ __align__(16) uint32_t unit[kRows * kStep * 4];
-    __shared__ uint32_t scale[2][kScaleSteps * kStep / 4][kRows];   // of these steps and the next ones
+__global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
+                                                                                      const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb,
+                                                                                      int64_t N, int W, int tiles_m, int tiles_n, float *__restrict__ out) {
+    constexpr int kRowsA = 64 * kA, kRowsB = 64 * kB, kRows = kRowsA + kRowsB, kPieces = kRows / kThreads;   // of 16 bytes of scales
+    static_assert(kScaleSteps * kStep == 16, "a piece is a row's scales of these steps");
+    // Codes of a step and of the next: block k of a row's eight is at place k ^ (row / 2 % 8) of the row, so that sixteen rows' blocks lie in
+    // different banks.
+    __shared__ __align__(16) uint32_t unit[2][kRows * kStep * 4];
+    __shared__ uint32_t scale[2][kScaleSteps * kStep / 4][kRows];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
 
     // Blocks of consecutive numbers go to the eight dies in turn: a die takes tiles that lie together, eight rows of tiles wide.
@@ -133,84 +145,98 @@ __global__ __launch_bounds__(kThreads, 2) void product_tiles_kernel(const uint32
     const uint32_t pitch = (uint32_t)W * kUnit;
     const int steps = (W + kStep - 1) / kStep;
 
-    // A wave's load fills eight rows of 128 bytes.  Rows and blocks past the end are taken from the last ones.
-    auto load = [&](int step) {
-        const uint32_t at = (uint32_t)min(step * kStep + ((lane & 7) ^ (lane >> 3)), W - 1) * kUnit;
-        load_rows<kRowsA>(a + m0 * W * 4, rows_a, pitch, at, wave, lane, unit);
-        load_rows<kRowsB>(b + n0 * W * 4, rows_b, pitch, at, wave, lane, unit + kRowsA * kStep * 4);
+    auto load = [&](int step) {   // (blocks past the row's end are taken from its last)
+        const uint32_t at = (uint32_t)min(step * kStep + ((lane & 7) ^ ((wave & 1) * 4 + (lane >> 4))), W - 1) * kUnit;
+        load_rows<kRowsA>(a + m0 * W * 4, rows_a, pitch, at, wave, lane, unit[step & 1]);
+        load_rows<kRowsB>(b + n0 * W * 4, rows_b, pitch, at, wave, lane, unit[step & 1] + kRowsA * kStep * 4);
     };
     uint32_t piece[kPieces][4];
     auto ask_scales = [&](int step) {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int p = anew(tid) + i * kThreads, r = p % kRows, at = step * kStep + p / kRows * 16;
+            const int r = anew(tid) + i * kThreads;
             const uint8_t *const row = r < kRowsA ? sa + (m0 + min(r, rows_a - 1)) * W : sb + (n0 + min(r - kRowsA, rows_b - 1)) * W;
-            scale_bytes<16>(row, at, W, piece[i]);
+            scale_bytes<16>(row, step * kStep, W, piece[i]);
         }
     };
     auto put_scales = [&](int step) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int p = anew(tid) + i * kThreads;
+        for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) scale[step / kScaleSteps % 2][p / kRows * 4 + j][p % kRows] = piece[i][j];
-        }
+            for (int j = 0; j < 4; ++j) scale[step / kScaleSteps & 1][j][anew(tid) + i * kThreads] = piece[i][j];
     };
 
     const int wm = (wave >> 1) * 32 * kA, wn = kRowsA + (wave & 1) * 32 * kB;   // this wave's rows
     v16f acc[kA][kB] = {};
-    v4u x[kA][4], y[kB][4];
-    uint32_t sx[kA], sy[kB];
-    auto take = [&](int t) {
-        const uint32_t *const from = unit + (col * kStep + ((4 * half + t) ^ (col & 7))) * 4;
+    v4u x[2][kA], y[2][kB];           // operands of a matrix instruction's dimensions, and of the next one's
+    uint32_t sx[2][kA], sy[2][kB];    // scales of a step, and of the next
+    auto take = [&](int step, int t) {
+        const uint32_t *const from = unit[step & 1] + (col * kStep + ((4 * half + t) ^ (col >> 1 & 7))) * 4;
 #pragma unroll
-        for (int i = 0; i < kA; ++i) x[i][t] = *reinterpret_cast<const v4u *>(from + (wm + i * 32) * kStep * 4);
+        for (int i = 0; i < kA; ++i) x[t & 1][i] = *reinterpret_cast<const v4u *>(from + (wm + i * 32) * kStep * 4);
 #pragma unroll
-        for (int i = 0; i < kB; ++i) y[i][t] = *reinterpret_cast<const v4u *>(from + (wn + i * 32) * kStep * 4);
+        for (int i = 0; i < kB; ++i) y[t & 1][i] = *reinterpret_cast<const v4u *>(from + (wn + i * 32) * kStep * 4);
+    };
+    auto take_scales = [&](int step, int to) {
+        const uint32_t *const from = scale[step / kScaleSteps & 1][step % kScaleSteps * 2 + half] + col;
+#pragma unroll
+        for (int i = 0; i < kA; ++i) sx[to][i] = from[wm + i * 32];
+#pragma unroll
+        for (int i = 0; i < kB; ++i) sy[to][i] = from[wn + i * 32];
     };
     auto multiply = [&](auto t_of) {
         constexpr int t = decltype(t_of)::value;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < kA; ++i)
 #pragma unroll
-            for (int j = 0; j < kB; ++j) acc[i][j] = mfma<t>(x[i][t], y[j][t], acc[i][j], sx[i], sy[j]);
+            for (int j = 0; j < kB; ++j) acc[i][j] = mfma<t>(x[t & 1][i], y[t & 1][j], acc[i][j], sx[0][i], sy[0][j]);
 #pragma unroll
-        for (int i = 0; i < kA; ++i)   // here, and not past the next barrier: operands take the registers of those that have been multiplied
+        for (int i = 0; i < kA; ++i)
 #pragma unroll
-            for (int j = 0; j < kB; ++j) acc[i][j] = anew(acc[i][j]);
+            for (int j = 0; j < kB; ++j) acc[i][j] = settled<(kA * kB > 8)>(acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
     };
+    // What a wave has asked for in LDS is there, for every wave, and what was there has been read by all.  (A barrier by itself does not wait for
+    // loads into LDS.)
+    auto meet = [&](int step) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (step * kStep + kStep > W) {   // blocks past the row's end: zeros
+            for (int u = tid; u < kRows * kStep; u += kThreads)
+                if (step * kStep + ((u & 7) ^ (u >> 4 & 7)) >= W) *reinterpret_cast<v4u *>(unit[step & 1] + u * 4) = v4u{0, 0, 0, 0};
+            __syncthreads();
+        }
+    };
+
     ask_scales(0);
     load(0);
     put_scales(0);
+    meet(0);
+    if (steps > 1) load(1);
+    take_scales(0, 0);
+    take(0, 0);
     for (int k = 0; k < steps; ++k) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // what this wave loads into LDS; the barrier alone does not wait for it
-        __syncthreads();
-        if (k * kStep + kStep > W) {   // blocks past the row's end: zeros
-            for (int u = tid; u < kRows * kStep; u += kThreads)
-                if (k * kStep + ((u & 7) ^ (u >> 3 & 7)) >= W) *reinterpret_cast<v4u *>(unit + u * 4) = v4u{0, 0, 0, 0};
-            __syncthreads();
-        }
-        take(0);
-        const uint32_t(*const scales)[kRows] = &scale[k / kScaleSteps % 2][k % kScaleSteps * 2 + half];
-#pragma unroll
-        for (int i = 0; i < kA; ++i) sx[i] = scales[0][wm + i * 32 + col];
-#pragma unroll
-        for (int i = 0; i < kB; ++i) sy[i] = scales[0][wn + i * 32 + col];
-        take(1);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(std::integral_constant<int, 0>{});
-        take(2);
-        take(3);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(std::integral_constant<int, 1>{});
-        __syncthreads();   // all operands are in registers
         const bool more = k + 1 < steps, scales_too = more && (k + 1) % kScaleSteps == 0;
         if (scales_too) ask_scales(k + 1);
-        if (more) load(k + 1);
-        multiply(std::integral_constant<int, 2>{});
-        multiply(std::integral_constant<int, 3>{});
+        take(k, 1);
+        multiply(std::integral_constant<int, 0>{});
+        take(k, 2);
+        multiply(std::integral_constant<int, 1>{});
+        take(k, 3);
         if (scales_too) put_scales(k + 1);
+        multiply(std::integral_constant<int, 2>{});
+        if (more) {
+            meet(k + 1);
+            if (k + 2 < steps) load(k + 2);
+            take_scales(k + 1, 1);
+            take(k + 1, 0);
+        }
+        multiply(std::integral_constant<int, 3>{});
+#pragma unroll
+        for (int i = 0; i < kA; ++i) sx[0][i] = sx[1][i];
+#pragma unroll
+        for (int i = 0; i < kB; ++i) sy[0][i] = sy[1][i];
     }
 #pragma unroll
     for (int i = 0; i < kA; ++i)
@@ -233,7 +259,7 @@ int launch_product_quantized(hdc_ctx_impl *c, const uint32_t *a, const uint8_t *
                              hipStream_t s) {
     ProfScope prof(c, HDC_K_PRODUCT_QUANTIZED, s);
     const int W = c->W;
-    const int64_t few = ((M + 31) / 32) * ((N + 31) / 32), large = ((M + 255) / 256) * ((N + 127) / 128), small = ((M + 127) / 128) * ((N + 127) / 128);
+    const int64_t few = ((M + 31) / 32) * ((N + 31) / 32), large = ((M + 255) / 256) * ((N + 255) / 256), small = ((M + 127) / 128) * ((N + 127) / 128);
     if (few < 4 * (int64_t)c->num_cus || N < 64 || M < 64) {
         const int steps = ((W + 2 * kFewWaves - 1) / (2 * kFewWaves) + 3) / 4 * 4;
         for (int64_t m = 0; m < M; m += 32 * 65535) {
@@ -242,8 +268,8 @@ int launch_product_quantized(hdc_ctx_impl *c, const uint32_t *a, const uint8_t *
                                sa + m * W, rows, b, sb, N, W, steps, out + m * N);
         }
     } else if (large >= c->num_cus) {
-        hipLaunchKernelGGL((product_tiles_kernel<4, 2>), dim3((unsigned)large), dim3(kThreads), 0, s, a, sa, M, b, sb, N, W, (int)((M + 255) / 256),
-                           (int)((N + 127) / 128), out);
+        hipLaunchKernelGGL((product_tiles_kernel<4, 4>), dim3((unsigned)large), dim3(kThreads), 0, s, a, sa, M, b, sb, N, W, (int)((M + 255) / 256),
+                           (int)((N + 255) / 256), out);
     } else {
         hipLaunchKernelGGL((product_tiles_kernel<2, 2>), dim3((unsigned)small), dim3(kThreads), 0, s, a, sa, M, b, sb, N, W, (int)((M + 127) / 128),
                            (int)((N + 127) / 128), out);

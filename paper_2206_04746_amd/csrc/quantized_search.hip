@@ -5,9 +5,9 @@
 // dimensions and holds the codes of its classes there in registers, so that all there is to read on the way is the samples, once.
 // The waves' parts of the dot products meet in LDS.
 //
-// Sums without rounding: the products of a wave are whole multiples of half the smallest scale, and 2 kSteps blocks of 32 dimensions give
-// at most 384 kSteps of the largest (32 times 6).  Where a row's scales within a wave's dimensions lie no further apart than
-// 2^kRange, that fits the 24 bits of the sums.  Where they lie further apart, the blocks are taken in several passes, each of the scales
+// Sums without rounding: the products of a row are whole multiples of half its smallest scale, and a block of 32 dimensions gives at
+// most 192 (32 times 6) of the largest.  Where a row's scales lie no further apart than 2^kRange, sums over it fit the 24 bits of
+// fp32, the waves' and theirs together.  Where they lie further apart, the blocks are taken in several passes, each of the scales
 // that lie within such a range, and the passes are added in fp64.
 #include <algorithm>
 
@@ -25,10 +25,10 @@ constexpr int kNoClass = 0x7FFFFFFF;
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
-// kSteps: matrix instructions of a wave, 64 dimensions each (a word of either half of the lanes).  Largest difference of scales.
-constexpr int range_of(int steps) {
+// The largest difference of scales of so many blocks.
+constexpr int range_of(int blocks) {
     int r = 0;
-    while ((int64_t)steps * 2 * 32 * 6 * 2 << (r + 1) <= 1 << 24) ++r;
+    while ((int64_t)blocks * 192 * 2 << (r + 1) <= 1 << 24) ++r;
     return r;
 }
 
@@ -52,6 +52,19 @@ struct Best {
 };
 __device__ __forceinline__ Best better(Best a, Best b) { return b.cos > a.cos || (b.cos == a.cos && b.c < a.c) ? b : a; }
 
+// The best of a row of 16 lanes, in each of them: neighbours, their neighbours, halves of eight, halves of the row.
+template <int kSel>
+__device__ __forceinline__ Best of_lane(Best b) {
+    auto from = [](int v) { return __builtin_amdgcn_update_dpp(0, v, kSel, 0xF, 0xF, true); };
+    return {__hiloint2double(from(__double2hiint(b.cos)), from(__double2loint(b.cos))), from(b.c)};
+}
+__device__ __forceinline__ Best best_of_16(Best b) {
+    b = better(b, of_lane<0xB1>(b));
+    b = better(b, of_lane<0x4E>(b));
+    b = better(b, of_lane<0x141>(b));
+    return better(b, of_lane<0x140>(b));
+}
+
 // grid (runs of `tiles` tiles of samples, splits of the groups of 32 classes).  kPart: part[n][C] takes the dot products; otherwise
 // cos_out (or null) the cosines, and the nearest class of a block's own goes to pred_out or, if that is null, to best_cos and best_c
 // [split][N].
@@ -61,12 +74,10 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
                                                                        const double *__restrict__ norm, double root_d, int tiles, int groups,
                                                                        double *__restrict__ part, float *__restrict__ cos_out,
                                                                        int32_t *__restrict__ pred_out, double *__restrict__ best_cos, int *__restrict__ best_c) {
-    constexpr int kRange = range_of(kSteps), kBlocks = kWaves * 2 * kSteps;   // of a row at a time
-    __shared__ float sums[2][kWaves][kTile][kTile + 1];
-    __shared__ double units[kWaves][kTile];
-    __shared__ int passes_of[kWaves];
-    __shared__ double near_cos[kWaves][kTile];
-    __shared__ int near_c[kWaves][kTile];
+    constexpr int kBlocks = kWaves * 2 * kSteps, kRange = range_of(kBlocks);   // of a row at a time
+    constexpr int kPitch = kTile + 4;                                          // (sixteen classes by four samples lie in different banks)
+    __shared__ float sums[2][kWaves][kTile][kPitch];
+    __shared__ int limits[2][kWaves][kTile];                    // largest and smallest scale of a class in a wave's dimensions
     __shared__ double run_cos[kPart ? 1 : kMaxTiles * kTile];   // the nearest of the groups before
     __shared__ int run_c[kPart ? 1 : kMaxTiles * kTile];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, col = lane & 31, half = lane >> 5;
@@ -76,7 +87,9 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
 
     v4u code[kSteps];
     uint32_t scale[kSteps / 4];   // a byte a step, less `top` (modulo 2^32, all four together): 127 for the row's largest
-    int top = 0, need = 1;        // the row's largest scale less 127; passes that the wave needs
+    int top = 0, passes = 1;      // the row's largest scale less 127; passes that the block needs
+    double unit[2], size[2];      // of this thread's two classes: the largest scale, the row's norm times that of a sample
+    const int n_of = tid >> 4, c_of = tid & 15;   // this thread's sample of a tile, and the first of its classes, which are 16 apart
     constexpr int kAhead = kSteps <= 20 ? 1 : 0;   // words of the next sample asked for before this one's products, or after them
     uint32_t word[1 + kAhead][kSteps];
 
@@ -123,12 +136,18 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
             most = max(most, s[t]);
             least = min(least, s[t] < 0 ? 256 : s[t]);
         }
-        most = max(most, __shfl_xor(most, 32, kWave));
+        constexpr int kNothing = 1 << 10;   // a block that is no number
+        most = max(none ? kNothing : most, __shfl_xor(none ? kNothing : most, 32, kWave));
         least = min(least, __shfl_xor(least, 32, kWave));
-        none |= (bool)__shfl_xor((int)none, 32, kWave);
-        need = most < 0 ? 1 : (most - least) / (kRange + 1) + 1;
-        for (int off = 1; off < 32; off <<= 1) need = max(need, __shfl_xor(need, off, kWave));
-        need = __builtin_amdgcn_readfirstlane(need);
+        __syncthreads();   // what is written here has been read
+        if (half == 0) limits[0][wave][col] = most, limits[1][wave][col] = least;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) most = max(most, limits[0][w][col]), least = min(least, limits[1][w][col]);
+        passes = most < 0 || most == kNothing ? 1 : (most - least) / (kRange + 1) + 1;
+        for (int off = 1; off < 32; off <<= 1) passes = max(passes, __shfl_xor(passes, off, kWave));
+        passes = __builtin_amdgcn_readfirstlane(passes);
+        most = most == kNothing ? kQuantZero : most;
         top = most - kQuantZero;
 #pragma unroll
         for (int t = 0; t < kSteps; t += 4) {   // (blocks of zeros as the largest)
@@ -137,15 +156,21 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
             for (int j = 0; j < 4; ++j) scale[t / 4] |= (uint32_t)(s[t + j] < 0 ? max(most, 0) : s[t + j]) << 8 * j;
             scale[t / 4] -= 0x01010101u * (uint32_t)top;
         }
-        __syncthreads();   // what is written here has been read
-        if (lane == 0) passes_of[wave] = need;
-        if (half == 0) units[wave][col] = none ? scale_value(kQuantNone) : most < 0 ? 1.0 : scale_value(most);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            int largest = -1;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) largest = max(largest, limits[0][w][c_of + 16 * j]);
+            unit[j] = largest == kNothing ? scale_value(kQuantNone) : largest < 0 ? 1.0 : scale_value(largest);
+        }
     };
 
     int turn = 0;
     ask(0, 0, word[0]);
     for (int g = g0; g < g1; ++g) {
-        const int n_of = tid & 31, c_of = g * kTile + (tid >> 5) * 2;   // this thread's sample and classes of a tile
+        const int c = g * kTile + c_of;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) size[j] = kPart || c + 16 * j >= C ? 0.0 : sqrt(norm[c + 16 * j]) * root_d;
         for (int i = 0; i < count; ++i) {
             double total[2] = {0.0, 0.0};
             for (int z = 0; z < parts; ++z) {
@@ -153,12 +178,12 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
                 const bool last = z + 1 == parts;
                 if (kAhead) ask(last ? (i + 1 < count ? i + 1 : 0) : i, last ? 0 : z + 1, word[kAhead]);
                 double down = 1.0;
-                for (int p = 0, passes = 1; p < passes; ++p) {
+                for (int p = 0; p < passes; ++p) {
                     v16f acc = {};
 #pragma unroll
                     for (int t = 0; t < kSteps; ++t) word[0][t] = anew(word[0][t]);   // (or all signs would be made before the loop)
                     top = anew(top);
-                    if (__builtin_expect(need == 1 && p == 0, 1)) {
+                    if (__builtin_expect(passes == 1, 1)) {
 #pragma unroll
                         for (int t = 0; t < kSteps; t += 4) {
                             acc = mfma<0>(code[t], signs_of(word[0][t]), acc, scale[t / 4]);
@@ -176,16 +201,16 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
                             __builtin_amdgcn_sched_barrier(0);
                         }
                     }
-                    float(*const to)[kTile + 1] = sums[turn][wave];
+                    float(*const to)[kPitch] = sums[turn][wave];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) to[8 * (j / 4) + 4 * half + j % 4][col] = acc[j];
                     __syncthreads();
-#pragma unroll 4
-                    for (int w = 0; w < kWaves; ++w) {
-                        passes = max(passes, passes_of[w]);
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            total[j] = fma((double)sums[turn][w][(tid >> 5) * 2 + j][n_of], units[w][(tid >> 5) * 2 + j] * down, total[j]);
+                    for (int j = 0; j < 2; ++j) {
+                        float sum = 0.0f;   // without rounding
+#pragma unroll
+                        for (int w = 0; w < kWaves; ++w) sum += sums[turn][w][c_of + 16 * j][n_of];
+                        total[j] = fma((double)sum, unit[j] * down, total[j]);
                     }
                     turn ^= 1;
                     down *= 1.0 / (2 << kRange);
@@ -201,25 +226,22 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
             if constexpr (kPart) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    if (n < N && c_of + j < C) part[n * C + c_of + j] = total[j];
+                    if (n < N && c + 16 * j < C) part[n * C + c + 16 * j] = total[j];
             } else {
                 Best best = {-__builtin_inf(), kNoClass};
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    if (c_of + j < C) {
-                        const double of = norm[c_of + j], cs = of == 0.0 ? 0.0 : total[j] / (sqrt(of) * root_d);
-                        if (cos_out && n < N) cos_out[n * C + c_of + j] = (float)cs;
-                        best = better(best, Best{cs, c_of + j});
+                    if (c + 16 * j < C) {
+                        const double cs = size[j] == 0.0 ? 0.0 : total[j] / size[j];
+                        if (cos_out && n < N) cos_out[n * C + c + 16 * j] = (float)cs;
+                        best = better(best, Best{cs, c + 16 * j});
                     }
-                best = better(best, Best{__shfl_xor(best.cos, 32, kWave), __shfl_xor(best.c, 32, kWave)});
-                if (half == 0) near_cos[wave][col] = best.cos, near_c[wave][col] = best.c;
-                __syncthreads();
-                if (tid < kTile) {
-                    if (g > g0) best = better(Best{run_cos[i * kTile + col], run_c[i * kTile + col]}, best);
-#pragma unroll
-                    for (int w = 1; w < kWaves; ++w) best = better(best, Best{near_cos[w][col], near_c[w][col]});
+                best = best_of_16(best);
+                if (c_of == 0) {
+                    const int at = i * kTile + n_of;
+                    if (g > g0) best = better(Best{run_cos[at], run_c[at]}, best);
                     if (g + 1 < g1) {
-                        run_cos[i * kTile + col] = best.cos, run_c[i * kTile + col] = best.c;
+                        run_cos[at] = best.cos, run_c[at] = best.c;
                     } else if (n < N) {
                         if (pred_out) {
                             pred_out[n] = best.c == kNoClass ? 0 : best.c;

@@ -260,6 +260,18 @@ def test_products_of_quantised_rows(M, N, D, kind):
     assert np.all(np.abs(got - want) <= (D + 2) * 2.0 ** -24 * size)
 
 
+# tiles of 128 and of 256 rows through LDS, with rows and dimensions past their ends
+@pytest.mark.parametrize("M,N,D", [(1100, 1000, 33), (1025, 1030, 1000), (900, 2100, 256), (4200, 4000, 250), (4097, 4097, 31), (3900, 4300, 2081), (64, 33000, 512)])
+def test_products_of_many_rows(M, N, D):
+    rng = np.random.default_rng(M + N * 3 + D * 11)
+    xa, xb = rows_of("normal", M, D, rng), rows_of("normal", N, D, rng)
+    xa[M // 2, D // 2] = np.nan
+    got, want, size = check_product(xa, xb)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    ok = ~np.isnan(want)
+    assert np.all(np.abs(got - want)[ok] <= (D + 2) * 2.0 ** -24 * size[ok])
+
+
 def test_products_with_blocks_that_are_no_number():
     rng = np.random.default_rng(8)
     got, want, _ = check_product(rows_of("none", 40, 300, rng), rows_of("none", 50, 300, rng))

@@ -68,7 +68,7 @@ __device__ __forceinline__ Best best_of_16(Best b) {
 // grid (runs of `tiles` tiles of samples, splits of the groups of 32 classes).  kPart: part[n][C] takes the dot products; otherwise
 // cos_out (or null) the cosines, and the nearest class of a block's own goes to pred_out or, if that is null, to best_cos and best_c
 // [split][N].
-template <int kSteps, bool kPart>
+template <int kSteps, bool kParts, bool kPart>
 __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uint32_t *__restrict__ hv, int64_t N, int W, int C,
                                                                        const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                                        const double *__restrict__ norm, double root_d, int tiles, int groups,
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     __shared__ int run_c[kPart ? 1 : kMaxTiles * kTile];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, col = lane & 31, half = lane >> 5;
     const int64_t all = (N + kTile - 1) / kTile, tile0 = (int64_t)blockIdx.x * tiles;
-    const int count = (int)min((int64_t)tiles, all - tile0), parts = (W + kBlocks - 1) / kBlocks;
+    const int count = (int)min((int64_t)tiles, all - tile0), parts = kParts ? (W + kBlocks - 1) / kBlocks : 1;
     const int g0 = blockIdx.y * groups, g1 = min(g0 + groups, (C + kTile - 1) / kTile);
 
     v4u code[kSteps];
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     int top = 0, passes = 1;      // the row's largest scale less 127; passes that the block needs
     double unit[2], size[2];      // of this thread's two classes: the largest scale, the row's norm times that of a sample
     const int n_of = tid >> 4, c_of = tid & 15;   // this thread's sample of a tile, and the first of its classes, which are 16 apart
-    constexpr int kAhead = kSteps <= 20 ? 1 : 0;   // words of the next sample asked for before this one's products, or after them
+    constexpr int kAhead = !kParts && kSteps <= 20 ? 1 : 0;   // words of the next sample asked for before this one's products, or after them
     uint32_t word[1 + kAhead][kSteps];
 
     // Words of sample tile i in part z of the row.  (Past the row's end, where the codes are zero, any word does.)
@@ -100,41 +100,54 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         if (w0 + 2 * kSteps <= W) {
             __builtin_memcpy(to, hv + n * W + first, sizeof(to));
         } else {
-            const uint32_t *const at = hv + anew(n * W);
+            const uint32_t *const at = hv + n * W;
+            const int here = anew(first);   // (no places in the row are kept)
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) {
-                to[t] = at[min(first + t, W - 1)];
+                to[t] = at[min(here + t, W - 1)];
                 if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (not all addresses at once)
             }
         }
     };
-    // This wave's codes of a group of classes in part z.
+    // This wave's codes of a group of classes in part z.  (Classes past the last are that one again.)
     auto hold = [&](int group, int z) {
-        const int c = group * kTile + col, first = z * kBlocks + (wave * 2 + half) * kSteps;
-        int s[kSteps], most = -1, least = 256;
-        bool none = false;
-        const int64_t from = anew((int64_t)min(c, C - 1) * W);
+        const int w0 = z * kBlocks + wave * 2 * kSteps, first = w0 + half * kSteps;
+        const int64_t from = anew((int64_t)min(group * kTile + col, C - 1) * W);
         const v4u *const here = reinterpret_cast<const v4u *>(codes) + from;
-        if (first - half * kSteps + 2 * kSteps <= W) {
+        if (w0 + 2 * kSteps <= W) {
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) code[t] = here[first + t];
-#pragma unroll
-            for (int t = 0; t < kSteps; ++t) s[t] = scales[from + first + t];
+            __builtin_memcpy(scale, scales + from + first, sizeof(scale));
         } else {
+            const int begin = anew(first);
 #pragma unroll
-            for (int t = 0; t < kSteps; ++t) {
-                code[t] = here[min(first + t, W - 1)];
-                s[t] = scales[from + min(first + t, W - 1)];
-                if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            for (int t = 0; t < kSteps; t += 4) {
+                scale[t / 4] = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int w = begin + t + j;
+                    code[t + j] = here[min(w, W - 1)];
+                    const uint32_t s = scales[from + min(w, W - 1)];
+                    if (w >= W) code[t + j] = v4u{0, 0, 0, 0};
+                    scale[t / 4] |= (w < W ? s : kQuantZero) << 8 * j;
+                }
+                __builtin_amdgcn_sched_barrier(0);   // (not all addresses at once)
             }
         }
+        // Blocks of zeros count for nothing, and neither do those that are no number: marked by a scale of 255, and codes of zero.
+        int most = -1, least = 256;
+        bool none = false;
 #pragma unroll
         for (int t = 0; t < kSteps; ++t) {
-            if (c >= C || first + t >= W) code[t] = v4u{0, 0, 0, 0}, s[t] = kQuantZero;
-            if (s[t] == kQuantNone) code[t] = v4u{0, 0, 0, 0}, none = true;
-            if (((code[t][0] | code[t][1] | code[t][2] | code[t][3]) & 0x77777777u) == 0) s[t] = -1;   // counts for nothing
-            most = max(most, s[t]);
-            least = min(least, s[t] < 0 ? 256 : s[t]);
+            const int s = scale[t / 4] >> 8 * (t & 3) & 255;
+            none |= s == kQuantNone;
+            const uint32_t any = (code[t][0] | code[t][1] | code[t][2] | code[t][3]) & 0x77777777u;
+            const bool counts = any != 0 && s != kQuantNone;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) code[t][r] = counts ? code[t][r] : 0u;
+            scale[t / 4] |= counts ? 0u : 255u << 8 * (t & 3);
+            most = max(most, counts ? s : -1);
+            least = min(least, counts ? s : 256);
         }
         constexpr int kNothing = 1 << 10;   // a block that is no number
         most = max(none ? kNothing : most, __shfl_xor(none ? kNothing : most, 32, kWave));
@@ -150,11 +163,14 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         most = most == kNothing ? kQuantZero : most;
         top = most - kQuantZero;
 #pragma unroll
-        for (int t = 0; t < kSteps; t += 4) {   // (blocks of zeros as the largest)
-            scale[t / 4] = 0;
+        for (int t = 0; t < kSteps; t += 4) {   // (marked ones as the largest)
+            uint32_t of = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) scale[t / 4] |= (uint32_t)(s[t + j] < 0 ? max(most, 0) : s[t + j]) << 8 * j;
-            scale[t / 4] -= 0x01010101u * (uint32_t)top;
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t s = scale[t / 4] >> 8 * j & 255;
+                of |= (s == kQuantNone ? (uint32_t)max(most, 0) : s) << 8 * j;
+            }
+            scale[t / 4] = of - 0x01010101u * (uint32_t)top;
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -165,93 +181,125 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         }
     };
 
-    int turn = 0;
+    // This wave's part of a tile's dot products, where the codes need one pass.
+    auto multiply = [&]() {
+        v16f acc = {};
+#pragma unroll
+        for (int t = 0; t < kSteps; t += 4) {
+            acc = mfma<0>(code[t], signs_of(word[0][t]), acc, scale[t / 4]);
+            acc = mfma<1>(code[t + 1], signs_of(word[0][t + 1]), acc, scale[t / 4]);
+            acc = mfma<2>(code[t + 2], signs_of(word[0][t + 2]), acc, scale[t / 4]);
+            acc = mfma<3>(code[t + 3], signs_of(word[0][t + 3]), acc, scale[t / 4]);
+            __builtin_amdgcn_sched_barrier(0);   // (not all signs at once: their registers)
+        }
+        return acc;
+    };
+    auto put = [&](int turn, v16f acc) {
+        float(*const to)[kPitch] = sums[turn][wave];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) to[8 * (j / 4) + 4 * half + j % 4][col] = acc[j];
+    };
+    auto sum_of = [&](int turn, int j) {
+        float sum = 0.0f;   // without rounding
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) sum += sums[turn][w][c_of + 16 * j][n_of];
+        return sum;
+    };
+    auto finish = [&](int g, int i, const double(&total)[2]) {
+        const int c = g * kTile + c_of;
+        const int64_t n = (tile0 + i) * kTile + n_of;
+        if constexpr (kPart) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (n < N && c + 16 * j < C) part[n * C + c + 16 * j] = total[j];
+        } else {
+            Best best = {-__builtin_inf(), kNoClass};
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (c + 16 * j < C) {
+                    const double cs = size[j] == 0.0 ? 0.0 : total[j] / size[j];
+                    if (cos_out && n < N) cos_out[n * C + c + 16 * j] = (float)cs;
+                    best = better(best, Best{cs, c + 16 * j});
+                }
+            best = best_of_16(best);
+            if (c_of == 0) {
+                const int at = i * kTile + n_of;
+                if (g > g0) best = better(Best{run_cos[at], run_c[at]}, best);
+                if (g + 1 < g1) {
+                    run_cos[at] = best.cos, run_c[at] = best.c;
+                } else if (n < N) {
+                    if (pred_out) {
+                        pred_out[n] = best.c == kNoClass ? 0 : best.c;
+                    } else {
+                        best_cos[(int64_t)blockIdx.y * N + n] = best.cos;
+                        best_c[(int64_t)blockIdx.y * N + n] = best.c;
+                    }
+                }
+            }
+        }
+    };
+
     ask(0, 0, word[0]);
     for (int g = g0; g < g1; ++g) {
-        const int c = g * kTile + c_of;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) size[j] = kPart || c + 16 * j >= C ? 0.0 : sqrt(norm[c + 16 * j]) * root_d;
+        for (int j = 0; j < 2; ++j) size[j] = kPart || g * kTile + c_of + 16 * j >= C ? 0.0 : sqrt(norm[g * kTile + c_of + 16 * j]) * root_d;
+        if constexpr (!kParts) {
+            hold(g, 0);
+            if (__builtin_expect(passes == 1, 1)) {
+                // A tile is finished while the next one's products are formed, by half of the waves before and by the other half after their own:
+                // of the two waves that share a SIMD one multiplies while the other adds.
+                const int one = anew(1);   // (no loop of its own for the first tile)
+                for (int i = 0; i <= count; ++i) {
+                    auto before = [&]() {
+                        const double total[2] = {(double)sum_of((i - 1) & 1, 0) * unit[0], (double)sum_of((i - 1) & 1, 1) * unit[1]};
+                        finish(g, i - 1, total);
+                    };
+                    if (i >= one && wave < kWaves / 2) before();
+                    if (i < count) {
+                        if constexpr (kAhead) ask(i + 1 < count ? i + 1 : 0, 0, word[kAhead]);
+                        put(i & 1, multiply());
+                        if constexpr (kAhead) {
+#pragma unroll
+                            for (int t = 0; t < kSteps; ++t) word[0][t] = word[kAhead][t];
+                        } else {
+                            ask(i + 1 < count ? i + 1 : 0, 0, word[0]);
+                        }
+                    }
+                    if (i >= one && wave >= kWaves / 2) before();
+                    if (i < count) __syncthreads();
+                }
+                continue;
+            }
+        }
+        int turn = 0;
         for (int i = 0; i < count; ++i) {
             double total[2] = {0.0, 0.0};
             for (int z = 0; z < parts; ++z) {
-                if (parts > 1 || i == 0) hold(g, z);
-                const bool last = z + 1 == parts;
-                if (kAhead) ask(last ? (i + 1 < count ? i + 1 : 0) : i, last ? 0 : z + 1, word[kAhead]);
+                if constexpr (kParts) hold(g, z);
                 double down = 1.0;
-                for (int p = 0; p < passes; ++p) {
+                for (int p = 0; p < passes; ++p) {   // the blocks whose scale is one of this pass's: from 2^-(kRange + 1) p of the largest on downwards
                     v16f acc = {};
 #pragma unroll
                     for (int t = 0; t < kSteps; ++t) word[0][t] = anew(word[0][t]);   // (or all signs would be made before the loop)
                     top = anew(top);
-                    if (__builtin_expect(passes == 1, 1)) {
 #pragma unroll
-                        for (int t = 0; t < kSteps; t += 4) {
-                            acc = mfma<0>(code[t], signs_of(word[0][t]), acc, scale[t / 4]);
-                            acc = mfma<1>(code[t + 1], signs_of(word[0][t + 1]), acc, scale[t / 4]);
-                            acc = mfma<2>(code[t + 2], signs_of(word[0][t + 2]), acc, scale[t / 4]);
-                            acc = mfma<3>(code[t + 3], signs_of(word[0][t + 3]), acc, scale[t / 4]);
-                            __builtin_amdgcn_sched_barrier(0);   // (not all signs at once: their registers)
-                        }
-                    } else {   // the blocks whose scale is one of this pass's: from 2^-(kRange + 1) p of the largest on downwards
-#pragma unroll
-                        for (int t = 0; t < kSteps; ++t) {
-                            const int of = (int)((scale[t / 4] + 0x01010101u * (uint32_t)top) >> 8 * (t & 3) & 255) - top + (kRange + 1) * p;
-                            const uint32_t mine = of <= kQuantZero && of >= kQuantZero - kRange ? ~0u : 0u;
-                            acc = mfma<0>(code[t] & mine, signs_of(word[0][t]), acc, (uint32_t)of & mine);
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
+                    for (int t = 0; t < kSteps; ++t) {
+                        const int of = (int)((scale[t / 4] + 0x01010101u * (uint32_t)top) >> 8 * (t & 3) & 255) - top + (kRange + 1) * p;
+                        const uint32_t mine = of <= kQuantZero && of >= kQuantZero - kRange ? ~0u : 0u;
+                        acc = mfma<0>(code[t] & mine, signs_of(word[0][t]), acc, (uint32_t)of & mine);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
-                    float(*const to)[kPitch] = sums[turn][wave];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) to[8 * (j / 4) + 4 * half + j % 4][col] = acc[j];
+                    put(turn, acc);
                     __syncthreads();
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        float sum = 0.0f;   // without rounding
-#pragma unroll
-                        for (int w = 0; w < kWaves; ++w) sum += sums[turn][w][c_of + 16 * j][n_of];
-                        total[j] = fma((double)sum, unit[j] * down, total[j]);
-                    }
+                    for (int j = 0; j < 2; ++j) total[j] = fma((double)sum_of(turn, j), unit[j] * down, total[j]);
                     turn ^= 1;
                     down *= 1.0 / (2 << kRange);
                 }
-                if constexpr (kAhead) {
-#pragma unroll
-                    for (int t = 0; t < kSteps; ++t) word[0][t] = word[kAhead][t];
-                } else {
-                    ask(last ? (i + 1 < count ? i + 1 : 0) : i, last ? 0 : z + 1, word[0]);
-                }
+                const bool last = z + 1 == parts;
+                ask(last ? (i + 1 < count ? i + 1 : 0) : i, last ? 0 : z + 1, word[0]);
             }
-            const int64_t n = (tile0 + i) * kTile + n_of;
-            if constexpr (kPart) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    if (n < N && c + 16 * j < C) part[n * C + c + 16 * j] = total[j];
-            } else {
-                Best best = {-__builtin_inf(), kNoClass};
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    if (c + 16 * j < C) {
-                        const double cs = size[j] == 0.0 ? 0.0 : total[j] / size[j];
-                        if (cos_out && n < N) cos_out[n * C + c + 16 * j] = (float)cs;
-                        best = better(best, Best{cs, c + 16 * j});
-                    }
-                best = best_of_16(best);
-                if (c_of == 0) {
-                    const int at = i * kTile + n_of;
-                    if (g > g0) best = better(Best{run_cos[at], run_c[at]}, best);
-                    if (g + 1 < g1) {
-                        run_cos[at] = best.cos, run_c[at] = best.c;
-                    } else if (n < N) {
-                        if (pred_out) {
-                            pred_out[n] = best.c == kNoClass ? 0 : best.c;
-                        } else {
-                            best_cos[(int64_t)blockIdx.y * N + n] = best.cos;
-                            best_c[(int64_t)blockIdx.y * N + n] = best.c;
-                        }
-                    }
-                }
-            }
+            finish(g, i, total);
         }
     }
 }
@@ -265,27 +313,23 @@ __global__ __launch_bounds__(256) void nearest_kernel(const double *__restrict__
     pred[n] = best.c == kNoClass ? 0 : best.c;
 }
 
-// Steps of a wave: as many as a row needs, up to 32 (the registers) at a time.
-int steps_of(int W) {
-    const int parts = (W + kWaves * 64 - 1) / (kWaves * 64), per = (W + parts - 1) / parts;
-    return ((per + kWaves * 2 - 1) / (kWaves * 2) + 3) / 4 * 4;
-}
-
 template <bool kPart>
 void launch(hdc_ctx_impl *c, dim3 grid, hipStream_t s, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
             int tiles, int groups, double *part, float *cos_out, int32_t *pred, double *best_cos, int *best_c) {
-#define HDC_SEARCH(STEPS)                                                                                                                                \
-    hipLaunchKernelGGL((search_quantized_kernel<STEPS, kPart>), grid, dim3(kThreads), 0, s, hv, N, c->W, c->p.C, codes, scales, norm, sqrt((double)c->p.D), \
+#define HDC_SEARCH(STEPS, PARTS)                                                                                                                             \
+    hipLaunchKernelGGL((search_quantized_kernel<STEPS, PARTS, kPart>), grid, dim3(kThreads), 0, s, hv, N, c->W, c->p.C, codes, scales, norm, sqrt((double)c->p.D), \
                        tiles, groups, part, cos_out, pred, best_cos, best_c)
-    switch (steps_of(c->W)) {
-        case 4: HDC_SEARCH(4); break;
-        case 8: HDC_SEARCH(8); break;
-        case 12: HDC_SEARCH(12); break;
-        case 16: HDC_SEARCH(16); break;
-        case 20: HDC_SEARCH(20); break;
-        case 24: HDC_SEARCH(24); break;
-        case 28: HDC_SEARCH(28); break;
-        default: HDC_SEARCH(32); break;
+    // Steps of a wave: as many as a row needs, up to 28 (the registers); rows of more than that go in parts of 16.
+    const int steps = ((c->W + kWaves * 2 - 1) / (kWaves * 2) + 3) / 4 * 4;
+    switch (steps) {
+        case 4: HDC_SEARCH(4, false); break;
+        case 8: HDC_SEARCH(8, false); break;
+        case 12: HDC_SEARCH(12, false); break;
+        case 16: HDC_SEARCH(16, false); break;
+        case 20: HDC_SEARCH(20, false); break;
+        case 24: HDC_SEARCH(24, false); break;
+        case 28: HDC_SEARCH(28, false); break;
+        default: HDC_SEARCH(16, true); break;
     }
 #undef HDC_SEARCH
 }

@@ -93,91 +93,92 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     constexpr int kAhead = !kParts && kSteps <= 20 ? 1 : 0;   // words of the next sample asked for before this one's products, or after them
     uint32_t word[1 + kAhead][kSteps];
 
+    // Step t has block 8 (t / 4) + 4 half + t % 4 of the wave's: a load of four words is 32 bytes of 32 rows.
     // Words of sample tile i in part z of the row.  (Past the row's end, where the codes are zero, any word does.)
     auto ask = [&](int i, int z, uint32_t(&to)[kSteps]) {
         const int64_t n = min((tile0 + i) * kTile + col, N - 1);
-        const int w0 = z * kBlocks + wave * 2 * kSteps, first = w0 + half * kSteps;
+        const int w0 = z * kBlocks + wave * 2 * kSteps;
+        const uint32_t *const from = hv + n * W;
         if (w0 + 2 * kSteps <= W) {
-            __builtin_memcpy(to, hv + n * W + first, sizeof(to));
+#pragma unroll
+            for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&to[t], from + w0 + 2 * t + 4 * half, 16);
         } else {
-            const uint32_t *const at = hv + n * W;
-            const int here = anew(first);   // (no places in the row are kept)
+            const int here = anew(w0 + 4 * half);   // (no places in the row are kept)
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) {
-                to[t] = at[min(here + t, W - 1)];
+                to[t] = from[min(here + 8 * (t / 4) + t % 4, W - 1)];
                 if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (not all addresses at once)
             }
         }
     };
     // This wave's codes of a group of classes in part z.  (Classes past the last are that one again.)
     auto hold = [&](int group, int z) {
-        const int w0 = z * kBlocks + wave * 2 * kSteps, first = w0 + half * kSteps;
+        const int w0 = z * kBlocks + wave * 2 * kSteps;
         const int64_t from = anew((int64_t)min(group * kTile + col, C - 1) * W);
         const v4u *const here = reinterpret_cast<const v4u *>(codes) + from;
         if (w0 + 2 * kSteps <= W) {
 #pragma unroll
-            for (int t = 0; t < kSteps; ++t) code[t] = here[first + t];
-            __builtin_memcpy(scale, scales + from + first, sizeof(scale));
+            for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&scale[t / 4], scales + from + w0 + 2 * t + 4 * half, 4);
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) code[t] = here[w0 + 8 * (t / 4) + 4 * half + t % 4];
         } else {
-            const int begin = anew(first);
+            const int begin = anew(w0 + 4 * half);
+            uint32_t s[kSteps];
 #pragma unroll
-            for (int t = 0; t < kSteps; t += 4) {
-                scale[t / 4] = 0;
+            for (int t = 0; t < kSteps; ++t) {
+                const int w = min(begin + 8 * (t / 4) + t % 4, W - 1);
+                s[t] = scales[from + w];
+                code[t] = here[w];
+                if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (not all addresses at once)
+            }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int w = begin + t + j;
-                    code[t + j] = here[min(w, W - 1)];
-                    const uint32_t s = scales[from + min(w, W - 1)];
-                    if (w >= W) code[t + j] = v4u{0, 0, 0, 0};
-                    scale[t / 4] |= (w < W ? s : kQuantZero) << 8 * j;
-                }
-                __builtin_amdgcn_sched_barrier(0);   // (not all addresses at once)
+            for (int t = 0; t < kSteps; ++t) {
+                const bool in = begin + 8 * (t / 4) + t % 4 < W;
+                scale[t / 4] = (t % 4 ? scale[t / 4] : 0u) | (in ? s[t] : 0u) << 8 * (t % 4);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) code[t][r] = in ? code[t][r] : 0u;
             }
         }
-        // Blocks of zeros count for nothing, and neither do those that are no number: marked by a scale of 255, and codes of zero.
+        // Blocks of zeros, whose scale is 0 and may lie far from the others', count for nothing.
+        uint32_t zeros = 0;
+#pragma unroll
+        for (int t = 0; t < kSteps; t += 4) zeros |= (scale[t / 4] - 0x01010101u) & ~scale[t / 4] & 0x80808080u;
+        if (__ballot(zeros != 0) != 0) {
+            zeros = 0;
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t)
+                if ((scale[t / 4] >> 8 * (t & 3) & 255) == 0 && ((code[t][0] | code[t][1] | code[t][2] | code[t][3]) & 0x77777777u) == 0) zeros |= 1u << t;
+        }
         int most = -1, least = 256;
-        bool none = false;
 #pragma unroll
         for (int t = 0; t < kSteps; ++t) {
             const int s = scale[t / 4] >> 8 * (t & 3) & 255;
-            none |= s == kQuantNone;
-            const uint32_t any = (code[t][0] | code[t][1] | code[t][2] | code[t][3]) & 0x77777777u;
-            const bool counts = any != 0 && s != kQuantNone;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) code[t][r] = counts ? code[t][r] : 0u;
-            scale[t / 4] |= counts ? 0u : 255u << 8 * (t & 3);
-            most = max(most, counts ? s : -1);
-            least = min(least, counts ? s : 256);
+            most = max(most, zeros >> t & 1 ? -1 : s);
+            least = min(least, zeros >> t & 1 ? 256 : s);
         }
-        constexpr int kNothing = 1 << 10;   // a block that is no number
-        most = max(none ? kNothing : most, __shfl_xor(none ? kNothing : most, 32, kWave));
+        most = max(most, __shfl_xor(most, 32, kWave));
         least = min(least, __shfl_xor(least, 32, kWave));
         __syncthreads();   // what is written here has been read
         if (half == 0) limits[0][wave][col] = most, limits[1][wave][col] = least;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) most = max(most, limits[0][w][col]), least = min(least, limits[1][w][col]);
-        passes = most < 0 || most == kNothing ? 1 : (most - least) / (kRange + 1) + 1;
+        passes = most < 0 || most == kQuantNone ? 1 : (most - least) / (kRange + 1) + 1;   // (of a row that is no number, any)
         for (int off = 1; off < 32; off <<= 1) passes = max(passes, __shfl_xor(passes, off, kWave));
         passes = __builtin_amdgcn_readfirstlane(passes);
-        most = most == kNothing ? kQuantZero : most;
+        if (__ballot(zeros != 0) != 0) {   // blocks of zeros as the largest
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) scale[t / 4] |= (zeros >> t & 1 ? (uint32_t)max(most, 0) : 0u) << 8 * (t & 3);
+        }
         top = most - kQuantZero;
 #pragma unroll
-        for (int t = 0; t < kSteps; t += 4) {   // (marked ones as the largest)
-            uint32_t of = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t s = scale[t / 4] >> 8 * j & 255;
-                of |= (s == kQuantNone ? (uint32_t)max(most, 0) : s) << 8 * j;
-            }
-            scale[t / 4] = of - 0x01010101u * (uint32_t)top;
-        }
+        for (int t = 0; t < kSteps; t += 4) scale[t / 4] -= 0x01010101u * (uint32_t)top;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             int largest = -1;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) largest = max(largest, limits[0][w][c_of + 16 * j]);
-            unit[j] = largest == kNothing ? scale_value(kQuantNone) : largest < 0 ? 1.0 : scale_value(largest);
+            unit[j] = largest < 0 ? 1.0 : scale_value(largest);
         }
     };
 
@@ -242,9 +243,11 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     ask(0, 0, word[0]);
     for (int g = g0; g < g1; ++g) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) size[j] = kPart || g * kTile + c_of + 16 * j >= C ? 0.0 : sqrt(norm[g * kTile + c_of + 16 * j]) * root_d;
+        for (int j = 0; j < 2; ++j) size[j] = kPart ? 0.0 : norm[min(g * kTile + c_of + 16 * j, C - 1)];
+        if constexpr (!kParts) hold(g, 0);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) size[j] = sqrt(size[j]) * root_d;
         if constexpr (!kParts) {
-            hold(g, 0);
             if (__builtin_expect(passes == 1, 1)) {
                 // A tile is finished while the next one's products are formed, by half of the waves before and by the other half after their own:
                 // of the two waves that share a SIMD one multiplies while the other adds.

@@ -14,6 +14,7 @@
 
 #include "hdc_internal.h"
 #include "online_weight.h"
+#include "quantized.h"
 
 namespace hdc {
 
@@ -302,14 +303,8 @@ static int cosine_group(int C) {
 // Blocks [0, wblocks): cp lanes per sample finish the dot products (finish_cosines), cosines
 // against the frozen rows, prediction (lowest class among equals) and the two
 // weights, as a record per sample and, for few classes, also as a dense row of signed fp64
-// coefficients (+w_y at y, -w_p at a wrong prediction, 0 elsewhere).  Blocks from wblocks on do an unrelated job that needs no launch of its own: each
-// turns a tile of 64 samples x 32 words of hv into colmask, the 64-bit lane mask of dimension
-// group g of sample n stored group-major (or gw adjacent groups interleaved per sample), so
-// that the backward step, which works on one or a few groups of all samples, reads its masks
-// contiguously instead of 8 bytes out of every 4 W-byte row.
-constexpr int kTileSamples = 64;
-constexpr int kTileGroups = 16;
-
+// coefficients (+w_y at y, -w_p at a wrong prediction, 0 elsewhere).  Blocks from wblocks on do an unrelated job that needs no launch of its own,
+// transpose_tile.
 __global__ __launch_bounds__(256, 8) void online_weights_kernel(
     const double *__restrict__ part, int slices, int64_t nb, const int32_t *__restrict__ labels,
     const double *__restrict__ normpart, int G, int C, double root_d, float lr,
@@ -317,28 +312,11 @@ __global__ __launch_bounds__(256, 8) void online_weights_kernel(
     const uint32_t *__restrict__ hv, int W, uint64_t *__restrict__ colmask, int64_t ld, int gw,
     uint32_t *reset) {
     extern __shared__ double nrm[];   // [C] squared norms of the frozen rows
-    __shared__ uint32_t tile[kTileSamples][2 * kTileGroups + 1];
+    __shared__ TransposeTile tile;
     const int t = threadIdx.x;
     if (reset && blockIdx.x == 0 && t == 0) *reset = 0;   // the row counter of online_lists_kernel, which runs next
     if ((int)blockIdx.x >= wblocks) {
-        const int idx = blockIdx.x - wblocks;
-        const int stiles = (int)(ld / kTileSamples);
-        const int64_t ns = (int64_t)(idx % stiles) * kTileSamples;
-        const int g0 = (idx / stiles) * kTileGroups;
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            const int sm = r * 8 + (t >> 5), w = 2 * g0 + (t & 31);
-            tile[sm][t & 31] = (ns + sm < nb && w < W) ? hv[(ns + sm) * W + w] : 0u;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int gg = (t >> 6) + 4 * i, sm = t & 63;
-            const int g = g0 + gg;
-            if (g < G)   // layout [g / gw][n][g % gw]: gw = 1 is group-major, gw > 1 interleaves gw groups
-                colmask[((int64_t)(g / gw) * ld + ns + sm) * gw + g % gw] =
-                    (uint64_t)tile[sm][2 * gg] | ((uint64_t)tile[sm][2 * gg + 1] << 32);
-        }
+        transpose_tile<256>(tile, (int)blockIdx.x - wblocks, hv, nb, W, G, colmask, ld, gw);
         return;
     }
     // squared norm of row c: a wave per class, lanes stride over the groups (fixed order)
@@ -388,12 +366,15 @@ __global__ __launch_bounds__(256, 8) void online_weights_kernel(
 typedef const uint64_t __attribute__((address_space(4))) *kptr_u64;
 typedef const double __attribute__((address_space(4))) *kptr_f64;
 
-template <int CB>
+//
+// kQuant: the rows are answered with in 4 bits (hdc_train_online_quantized): on the last launch of a batch the elements are quantised as they
+// are updated, and normpart takes the squared norm of what they have become.
+template <int CB, bool kQuant>
 __global__ __launch_bounds__(kBwdMaxWaves *kWave) void online_bwd_kernel(
     const uint64_t *__restrict__ colmask, int64_t ld, const OnlineWeight *__restrict__ wts,
     const double *__restrict__ coef, int64_t nb, float *acc, int D, int c_lo, int c_n, int G,
     double *carry, int first, int last, double *__restrict__ normpart, int gpb, int64_t bs,
-    double *__restrict__ partial, int c_all) {
+    double *__restrict__ partial, int c_all, QuantRows quant, int W) {
     extern __shared__ double rows[];   // [waves][c_n][64]
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -518,11 +499,13 @@ __global__ __launch_bounds__(kBwdMaxWaves *kWave) void online_bwd_kernel(
             continue;
         }
         double q = 0.0;
+        float nv = 0.0f;
         if (d < D) {
-            const float nv = (float)((double)acc[at] + s);
+            nv = (float)((double)acc[at] + s);
             acc[at] = nv;
             q = (double)nv * (double)nv;
         }
+        if constexpr (kQuant) q = quantise_pair(quant, c_lo + c, 2 * g2, W, nv, lane);
         q = wave_sum_f64(q);
         if (lane == 0) normpart[(int64_t)(c_lo + c) * G + g2] = q;
     }
@@ -608,10 +591,11 @@ __global__ __launch_bounds__(kBwdMaxWaves *kWave) void online_bwd_wide_kernel(
 // delta = the blocks' shares in block order (plus the carry of earlier launches of the same
 // batch), then the update and the norm partials exactly as in online_bwd_kernel.
 // grid (G, ceil(C / 4)), one wave per (class, group).
+template <bool kQuant>
 __global__ __launch_bounds__(256) void online_apply_kernel(const double *__restrict__ partial, int shares,
                                                            float *acc, int D, int C, int G, double *carry,
                                                            int first, int last, double *__restrict__ normpart,
-                                                           const uint32_t *__restrict__ slots) {
+                                                           const uint32_t *__restrict__ slots, QuantRows quant, int W) {
     const int lane = threadIdx.x & (kWave - 1);
     const int c = blockIdx.y * 4 + (threadIdx.x >> 6), g = blockIdx.x;
     if (c >= C) return;
@@ -641,11 +625,13 @@ __global__ __launch_bounds__(256) void online_apply_kernel(const double *__restr
         return;
     }
     double q = 0.0;
+    float nv = 0.0f;
     if (d < D) {
-        const float nv = (float)((double)acc[at] + s);
+        nv = (float)((double)acc[at] + s);
         acc[at] = nv;
         q = (double)nv * (double)nv;
     }
+    if constexpr (kQuant) q = quantise_pair(quant, c, 2 * g, W, nv, lane);
     q = wave_sum_f64(q);
     if (lane == 0) normpart[(int64_t)c * G + g] = q;
 }
@@ -847,7 +833,8 @@ static bool bwd_by_lists(int C, int64_t nb) { return C > 16 && nb >= 1024; }
 constexpr int kListGroups = 4;   // dimension groups per wave of online_bwd_list_kernel
 static int64_t list_rows(int64_t nb, int C) { return 2 * nb / kListItem + C + 1; }   // most share rows
 
-static int launch_bwd(hdc_ctx_impl *c, int64_t ld, int64_t nb, float *acc, int G, bool first, bool last,
+template <bool kQuant>
+static int launch_bwd(hdc_ctx_impl *c, int64_t ld, int64_t nb, float *acc, int G, bool first, bool last, QuantRows quant,
                       hipStream_t s) {
     const int C = c->p.C;
     const OnlineWeight *wts = static_cast<const OnlineWeight *>(c->ob_wts_d);
@@ -859,9 +846,9 @@ static int launch_bwd(hdc_ctx_impl *c, int64_t ld, int64_t nb, float *acc, int G
                            dim3((unsigned)((G + kListGroups - 1) / kListGroups), (unsigned)list_rows(nb, C)),
                            dim3(kListWaves * kWave),
                            0, s, c->ob_col_d, ld, c->ob_ln_d, c->ob_lw_d, c->ob_meta_d, C, c->p.D, c->ob_share_d);
-        hipLaunchKernelGGL(online_apply_kernel, dim3((unsigned)G, (unsigned)((C + 3) / 4)), dim3(256), 0, s,
+        hipLaunchKernelGGL(online_apply_kernel<kQuant>, dim3((unsigned)G, (unsigned)((C + 3) / 4)), dim3(256), 0, s,
                            c->ob_share_d, 0, acc, c->p.D, C, G, c->ob_carry_d, first ? 1 : 0, last ? 1 : 0,
-                           c->ob_norm_d, c->ob_meta_d);
+                           c->ob_norm_d, c->ob_meta_d, quant, c->W);
         HDC_HIP(hipGetLastError());
         return HDC_OK;
     }
@@ -886,9 +873,9 @@ static int launch_bwd(hdc_ctx_impl *c, int64_t ld, int64_t nb, float *acc, int G
             }
 #undef HDC_BWD
             HDC_HIP(hipGetLastError());
-            hipLaunchKernelGGL(online_apply_kernel, dim3((unsigned)G, (unsigned)((C + 3) / 4)), dim3(256), 0, s,
+            hipLaunchKernelGGL(online_apply_kernel<kQuant>, dim3((unsigned)G, (unsigned)((C + 3) / 4)), dim3(256), 0, s,
                                c->ob_share_d, used, acc, c->p.D, C, G, c->ob_carry_d, first ? 1 : 0, last ? 1 : 0,
-                               c->ob_norm_d, static_cast<const uint32_t *>(nullptr));
+                               c->ob_norm_d, static_cast<const uint32_t *>(nullptr), quant, c->W);
         }
         HDC_HIP(hipGetLastError());
         return HDC_OK;
@@ -903,9 +890,9 @@ static int launch_bwd(hdc_ctx_impl *c, int64_t ld, int64_t nb, float *acc, int G
         const int64_t bs = (nb + kBwdUnroll - 1) / kBwdUnroll * kBwdUnroll;   // one block takes all samples
         ProfScope prof(c, HDC_K_ONLINE_BWD, s);
 #define HDC_BWD(CB)                                                                                          \
-    hipLaunchKernelGGL(online_bwd_kernel<CB>, grid, block, lds, s, c->ob_col_d, ld, wts, c->ob_coef_d, nb, acc, \
+    hipLaunchKernelGGL((online_bwd_kernel<CB, kQuant>), grid, block, lds, s, c->ob_col_d, ld, wts, c->ob_coef_d, nb, acc, \
                        c->p.D, c_lo, c_n, G, c->ob_carry_d, first ? 1 : 0, last ? 1 : 0, c->ob_norm_d, 1, bs,  \
-                       static_cast<double *>(nullptr), C)
+                       static_cast<double *>(nullptr), C, quant, c->W)
         switch (bwd_dense_width(C)) {
             case 2: HDC_BWD(2); break;
             case 4: HDC_BWD(4); break;
@@ -1031,13 +1018,7 @@ int reserve_search_cosine(hdc_ctx_impl *c, int64_t queries) {
     return rc;
 }
 
-// The rows that a call answers with in 4 bits (hdc_train_online_quantized).
-struct QuantRows {
-    uint32_t *codes;
-    uint8_t *scales;
-};
-
-// Batch after batch, each in pieces; `quant`, if not null, has the rows quantised before each and the samples scored against those.
+// Batch after batch, each in pieces; `quant`, if not null, has the rows quantised and the samples scored against what they have become.
 static int train_pieces(hdc_ctx_impl *c, const uint32_t *hv, const int32_t *labels, int64_t N, int32_t epochs, float lr, int64_t batch,
                         float *acc, const QuantRows *quant, hipStream_t s) {
     const int C = c->p.C, D = c->p.D, W = c->W;
@@ -1051,46 +1032,50 @@ static int train_pieces(hdc_ctx_impl *c, const uint32_t *hv, const int32_t *labe
     if (!quant) (void)online_chain_ready(c, s, &rc);   // (a longer call, or smaller batches, go in blocks)
     if (rc != HDC_OK) return rc;
     if (!c->ob_attr_set) {
-        const void *kernels[] = {reinterpret_cast<const void *>(online_bwd_kernel<0>),
-                                 reinterpret_cast<const void *>(online_bwd_kernel<2>),
-                                 reinterpret_cast<const void *>(online_bwd_kernel<4>),
-                                 reinterpret_cast<const void *>(online_bwd_kernel<8>),
-                                 reinterpret_cast<const void *>(online_bwd_kernel<16>)};
+#define HDC_BWD(CB) reinterpret_cast<const void *>(online_bwd_kernel<CB, false>), reinterpret_cast<const void *>(online_bwd_kernel<CB, true>)
+        const void *kernels[] = {HDC_BWD(0), HDC_BWD(2), HDC_BWD(4), HDC_BWD(8), HDC_BWD(16)};
+#undef HDC_BWD
         for (const void *k : kernels)
             HDC_HIP(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize,
                                         (int)(kBwdSlots * kWave * sizeof(double))));
         c->ob_attr_set = true;
     }
 
-    if (!quant) rc = launch_norm(c, acc, G, s);   // squared norms of the rows as handed in
+    // squared norms of the rows as handed in, or quantised; after that the updates see to both
+    rc = quant ? launch_quantize(c, acc, C, quant->codes, quant->scales, nullptr, c->ob_norm_d, s) : launch_norm(c, acc, G, s);
     if (rc != HDC_OK) return rc;
     const double root_d = sqrt((double)D);
     const int ttiles = (G + kTileGroups - 1) / kTileGroups;
     for (int32_t e = 0; e < epochs; ++e)
         for (int64_t b0 = 0; b0 < N; b0 += batch) {
             const int64_t B = b0 + batch < N ? batch : N - b0;
-            if (quant) rc = launch_quantize(c, acc, C, quant->codes, quant->scales, nullptr, c->ob_norm_d, s);
-            if (rc != HDC_OK) return rc;
             for (int64_t s0 = 0; s0 < B; s0 += sb) {
                 const int64_t nb = s0 + sb < B ? sb : B - s0;
                 const uint32_t *rows = hv + (b0 + s0) * W;
                 int slices;
-                rc = quant ? launch_quantized_dots(c, rows, nb, quant->codes, quant->scales, c->ob_part_d, &slices, s)
-                           : launch_fwd(c, rows, nb, acc, false, &slices, s);
-                if (rc != HDC_OK) return rc;
                 const int64_t ld_used = (nb + kTileSamples - 1) / kTileSamples * kTileSamples;
-                const int cp = cosine_group(C);
-                const int wblocks = (int)((ld_used + 256 / cp - 1) / (256 / cp));
                 const int tblocks = (int)(ld_used / kTileSamples) * ttiles;
-                hipLaunchKernelGGL(online_weights_kernel, dim3((unsigned)(wblocks + tblocks)), dim3(256),
-                                   (size_t)C * sizeof(double), s, c->ob_part_d, slices, nb, labels + b0 + s0,
-                                   c->ob_norm_d, G, C, root_d, lr, static_cast<OnlineWeight *>(c->ob_wts_d),
-                                   cb && !bwd_by_lists(C, nb) ? c->ob_coef_d : nullptr, cb, cp, wblocks, rows, W,
-                                   c->ob_col_d, ld_used,
-                                   bwd_by_lists(C, nb) ? kListGroups : bwd_shares(c, G, nb) > 1 ? bwd_group_width(C) : 1,
-                                   bwd_by_lists(C, nb) ? c->ob_meta_d + 3 * C : nullptr);
-                HDC_HIP(hipGetLastError());
-                rc = launch_bwd(c, ld_used, nb, acc, G, s0 == 0, s0 + nb == B, s);
+                const bool lists = bwd_by_lists(C, nb);
+                const QuantWeights out = {labels + b0 + s0, c->ob_norm_d, static_cast<OnlineWeight *>(c->ob_wts_d), cb && !lists ? c->ob_coef_d : nullptr,
+                                          c->ob_col_d, lists ? c->ob_meta_d + 3 * C : nullptr, ld_used, lr, G, cb,
+                                          lists ? kListGroups : bwd_shares(c, G, nb) > 1 ? bwd_group_width(C) : 1, tblocks};
+                if (quant && quantized_weights_takes(C, nb)) {
+                    rc = launch_quantized_weights(c, rows, nb, quant->codes, quant->scales, out, s);
+                    if (rc != HDC_OK) return rc;
+                } else {
+                    rc = quant ? launch_quantized_dots(c, rows, nb, quant->codes, quant->scales, c->ob_part_d, &slices, s)
+                               : launch_fwd(c, rows, nb, acc, false, &slices, s);
+                    if (rc != HDC_OK) return rc;
+                    const int cp = cosine_group(C);
+                    const int wblocks = (int)((ld_used + 256 / cp - 1) / (256 / cp));
+                    hipLaunchKernelGGL(online_weights_kernel, dim3((unsigned)(wblocks + tblocks)), dim3(256),
+                                       (size_t)C * sizeof(double), s, c->ob_part_d, slices, nb, out.labels,
+                                       c->ob_norm_d, G, C, root_d, lr, out.records, out.coef, cb, cp, wblocks, rows, W,
+                                       c->ob_col_d, ld_used, out.gw, out.reset);
+                    HDC_HIP(hipGetLastError());
+                }
+                rc = quant ? launch_bwd<true>(c, ld_used, nb, acc, G, s0 == 0, s0 + nb == B, *quant, s)
+                           : launch_bwd<false>(c, ld_used, nb, acc, G, s0 == 0, s0 + nb == B, QuantRows{}, s);
                 if (rc != HDC_OK) return rc;
             }
         }

@@ -14,6 +14,36 @@ struct OnlineWeight {
     float w_p;      // float(lr * (1 - cos_pred))
 };
 
+// The backward step's transposed sample bits: job `idx` of a batch turns a tile of 64 samples x 32 words of hv into colmask, the 64-bit lane
+// mask of dimension group g of sample n stored group-major (or gw adjacent groups interleaved per sample), so that the step,
+// which works on one or a few groups of all samples, reads its masks contiguously instead of 8 bytes out of every 4 W-byte row.  The
+// block's threads call it together.
+constexpr int kTileSamples = 64;
+constexpr int kTileGroups = 16;
+typedef uint32_t TransposeTile[kTileSamples][2 * kTileGroups + 1];
+
+template <int kThreads>
+__device__ __forceinline__ void transpose_tile(TransposeTile &tile, int idx, const uint32_t *__restrict__ hv, int64_t nb, int W, int G,
+                                               uint64_t *__restrict__ colmask, int64_t ld, int gw) {
+    const int t = threadIdx.x;
+    const int stiles = (int)(ld / kTileSamples);
+    const int64_t ns = (int64_t)(idx % stiles) * kTileSamples;
+    const int g0 = (idx / stiles) * kTileGroups;
+#pragma unroll
+    for (int r = 0; r < kTileSamples * 32 / kThreads; ++r) {
+        const int sm = r * (kThreads / 32) + (t >> 5), w = 2 * g0 + (t & 31);
+        tile[sm][t & 31] = (ns + sm < nb && w < W) ? hv[(ns + sm) * W + w] : 0u;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTileGroups * 64 / kThreads; ++i) {
+        const int gg = (t >> 6) + kThreads / 64 * i, sm = t & 63;
+        const int g = g0 + gg;
+        if (g < G)   // layout [g / gw][n][g % gw]: gw = 1 is group-major, gw > 1 interleaves gw groups
+            colmask[((int64_t)(g / gw) * ld + ns + sm) * gw + g % gw] = (uint64_t)tile[sm][2 * gg] | ((uint64_t)tile[sm][2 * gg + 1] << 32);
+    }
+}
+
 // A context-owned buffer of at least `want` bytes; a no-op when it is that large already.
 template <typename T>
 int grow(T **p, size_t *have, size_t want) {

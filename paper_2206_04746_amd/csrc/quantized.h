@@ -6,6 +6,7 @@
 #pragma once
 
 #include "hdc_internal.h"
+#include "online_weight.h"
 
 namespace hdc {
 
@@ -29,6 +30,69 @@ __device__ __forceinline__ T anew(T v) {
 // 2^(s - 127) in 64 bits; a quiet NaN for a block that is no number.
 __device__ __forceinline__ double scale_value(int s) {
     return s == kQuantNone ? __longlong_as_double(0x7FF8000000000000ll) : __longlong_as_double((long long)(s + 896) << 52);
+}
+
+// Lane exchanges within a row of 16: with the neighbour, with the neighbour's neighbour, and from the other end of eight lanes and of all.
+template <int kSel>
+__device__ __forceinline__ uint32_t lanes(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kSel, 0xF, 0xF, true);
+}
+constexpr int kNext = 0xB1, kNextPair = 0x4E, kMirrorEight = 0x141, kMirrorRow = 0x140;
+
+// The scale byte of a block whose largest magnitude has these bits (of a number), and its value.
+__device__ __forceinline__ int scale_of(uint32_t most) { return max((int)(most >> 23) - 2, 0); }   // floor(log2) less 2; what is below 2^-126: 2^-127
+__device__ __forceinline__ float scale_float(int s) { return __uint_as_float(s ? (uint32_t)s << 23 : 0x00400000u); }
+// A quarter of the square of a scale: what the square of a code's halves counts for.
+__device__ __forceinline__ double scale_square(int s) {
+    return s == kQuantNone ? scale_value(kQuantNone) : __longlong_as_double((long long)(2 * s + 1023 - 2 * kQuantZero - 2) << 52);
+}
+
+// Rows that are quantised as they are trained (online_batched.hip).
+struct QuantRows {
+    uint32_t *codes;
+    uint8_t *scales;
+};
+
+// What online_weights_kernel makes of a batch's dot products, made where these are formed: the samples' weight records and, for few classes,
+// their dense rows of signed weights (coef, width cb), and the transposed bits by blocks of their own.
+struct QuantWeights {
+    const int32_t *labels;
+    const double *normpart;   // [C][G]
+    OnlineWeight *records;
+    double *coef;
+    uint64_t *colmask;
+    uint32_t *reset;          // a counter to be zero afterwards, or null
+    int64_t ld;               // samples, up to a multiple of 64
+    float lr;
+    int G, cb, gw, tblocks;   // blocks for the transposed bits
+};
+bool quantized_weights_takes(int C, int64_t nb);
+int launch_quantized_weights(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const uint32_t *codes, const uint8_t *scales, const QuantWeights &out,
+                             hipStream_t s);
+
+// Two blocks of a row, w and w + 1 (if there is one), an element a lane: their codes by ballots of the codes' bits, their scales, and, in
+// every lane, what they add to the squared norm is to be summed from.
+__device__ __forceinline__ double quantise_pair(QuantRows to, int64_t c, int w, int W, float x, int lane) {
+    uint32_t most = __float_as_uint(x) & 0x7FFFFFFFu;
+    most = max(most, lanes<kNext>(most));
+    most = max(most, lanes<kNextPair>(most));
+    most = max(most, lanes<kMirrorEight>(most));
+    most = max(most, lanes<kMirrorRow>(most));
+    most = max(most, (uint32_t)__shfl_xor((int)most, 16, kWave));
+    const bool none = most >= 0x7F800000u;
+    const int s = none ? kQuantNone : scale_of(most);
+    const uint32_t code = none ? 0u : __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x, 0.0f, scale_float(s), 0) & 15u;
+    uint64_t bits[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) bits[k] = __ballot(code >> k & 1);
+    const int block = lane >> 2 & 1;
+    uint32_t word = 0;   // lane 4 b + r: word r of block b
+#pragma unroll
+    for (int k = 0; k < 4; ++k) word |= ((uint32_t)(bits[k] >> 32 * block) >> (lane & 3) & 0x11111111u) << k;
+    if (lane < 8 && w + block < W) to.codes[(c * W + w) * 4 + lane] = word;
+    if ((lane & 31) == 0 && w + (lane >> 5) < W) to.scales[c * W + w + (lane >> 5)] = (uint8_t)s;
+    const int halves = code_halves(code);
+    return (double)(halves * halves) * scale_square(s);
 }
 
 }  // namespace hdc

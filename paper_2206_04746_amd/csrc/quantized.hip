@@ -13,13 +13,6 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
-// Lane exchanges within a row of 16: with the neighbour, with the neighbour's neighbour, and among eight lanes from the other end.
-template <int kSel>
-__device__ __forceinline__ uint32_t lanes(uint32_t v) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kSel, 0xF, 0xF, true);
-}
-constexpr int kNext = 0xB1, kNextPair = 0x4E, kMirrorEight = 0x141;
-
 // Squares of the magnitudes in halves, by code: 0 1 4 9 16 36 64 144.
 __device__ __forceinline__ int squares(uint32_t four) {
     return (int)__builtin_amdgcn_udot4(__builtin_amdgcn_perm(0x90402410u, 0x09040100u, four & 0x07070707u), 0x01010101u, 0u, false);
@@ -61,8 +54,8 @@ __global__ __launch_bounds__(1024) void quantize_rows_kernel(const float *__rest
                 most = max(most, lanes<kNextPair>(most));
                 most = max(most, lanes<kMirrorEight>(most));
                 const bool none = most >= 0x7F800000u;
-                const int s = max((int)(most >> 23) - 2, 0);   // floor(log2) less 2; what is below 2^-126 has 2^-127
-                const float unit = __uint_as_float(s ? (uint32_t)s << 23 : 0x00400000u);
+                const int s = none ? kQuantNone : scale_of(most);
+                const float unit = scale_float(s);
                 uint32_t four = 0;
                 if (!none) {
                     four = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(four, __uint_as_float(x[k][0]), 0.0f, unit, 0);
@@ -70,9 +63,7 @@ __global__ __launch_bounds__(1024) void quantize_rows_kernel(const float *__rest
                     four = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(four, __uint_as_float(x[k][2]), 0.0f, unit, 2);
                     four = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(four, __uint_as_float(x[k][3]), 0.0f, unit, 3);
                 }
-                // a quarter of the square of the scale
-                const double square = none ? scale_value(kQuantNone) : __longlong_as_double((long long)(2 * s + 1023 - 2 * kQuantZero - 2) << 52);
-                mine = fma((double)squares(four), square, mine);
+                mine = fma((double)squares(four), scale_square(s), mine);
                 if (part) {   // sixteen lanes a group
                     for (int off = 1; off < 16; off <<= 1) mine += __shfl_xor(mine, off, kWave);
                     if ((lane & 15) == 0 && w < W) part[n * G + w / 2] = mine;
@@ -82,7 +73,7 @@ __global__ __launch_bounds__(1024) void quantize_rows_kernel(const float *__rest
                 four |= lanes<kNext>(four);
                 const uint32_t two = __builtin_amdgcn_perm(lanes<kNextPair>(four), four, pick);
                 word[k] = __builtin_amdgcn_perm(lanes<kNextPair>(lanes<kMirrorEight>(two)), two, half);
-                if (j == 0 && w < W) scales[n * W + w] = (uint8_t)(none ? kQuantNone : s);
+                if (j == 0 && w < W) scales[n * W + w] = (uint8_t)s;
             }
             const int w = w0 + 8 * (j & 1) + (lane >> 3);
             if (w < W) codes[(n * W + w) * 4 + pair] = word[j & 1];

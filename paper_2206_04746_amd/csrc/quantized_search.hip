@@ -10,6 +10,7 @@
 // fp32, the waves' and theirs together.  Where they lie further apart, the blocks are taken in several passes, each of the scales
 // that lie within such a range, and the passes are added in fp64.
 #include <algorithm>
+#include <type_traits>
 
 #include "online_weight.h"
 #include "quantized.h"
@@ -65,23 +66,47 @@ __device__ __forceinline__ Best best_of_16(Best b) {
     return better(b, of_lane<0x140>(b));
 }
 
-// grid (runs of `tiles` tiles of samples, splits of the groups of 32 classes).  kPart: part[n][C] takes the dot products; otherwise
-// cos_out (or null) the cosines, and the nearest class of a block's own goes to pred_out or, if that is null, to best_cos and best_c
-// [split][N].
-template <int kSteps, bool kParts, bool kPart>
+__device__ __forceinline__ double sum_of_16(double v) {
+    auto from = [](double x, auto sel) {
+        constexpr int kSel = decltype(sel)::value;
+        return __hiloint2double((int)lanes<kSel>((uint32_t)__double2hiint(x)), (int)lanes<kSel>((uint32_t)__double2loint(x)));
+    };
+    v += from(v, std::integral_constant<int, kNext>{});
+    v += from(v, std::integral_constant<int, kNextPair>{});
+    v += from(v, std::integral_constant<int, kMirrorEight>{});
+    return v + from(v, std::integral_constant<int, kMirrorRow>{});
+}
+
+// grid (runs of `tiles` tiles of samples, splits of the groups of 32 classes).
+//   kNearest  cos_out (or null) takes the cosines, and the nearest class of a block's own goes to pred_out or, if that is null, to best_cos and
+//             best_c [split][N]
+//   kDots     part[n][C] takes the dot products
+//   kWeights  up to 32 classes: the weights of online training (`weigh`); the last weigh.tblocks blocks transpose the samples' bits
+enum Mode { kNearest, kDots, kWeights };
+template <int kSteps, bool kParts, int kMode>
 __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uint32_t *__restrict__ hv, int64_t N, int W, int C,
                                                                        const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                                        const double *__restrict__ norm, double root_d, int tiles, int groups,
                                                                        double *__restrict__ part, float *__restrict__ cos_out,
-                                                                       int32_t *__restrict__ pred_out, double *__restrict__ best_cos, int *__restrict__ best_c) {
+                                                                       int32_t *__restrict__ pred_out, double *__restrict__ best_cos, int *__restrict__ best_c,
+                                                                       QuantWeights weigh) {
     constexpr int kBlocks = kWaves * 2 * kSteps, kRange = range_of(kBlocks);   // of a row at a time
     constexpr int kPitch = kTile + 4;                                          // (sixteen classes by four samples lie in different banks)
     __shared__ float sums[2][kWaves][kTile][kPitch];
     __shared__ int limits[2][kWaves][kTile];                    // largest and smallest scale of a class in a wave's dimensions
-    __shared__ double run_cos[kPart ? 1 : kMaxTiles * kTile];   // the nearest of the groups before
-    __shared__ int run_c[kPart ? 1 : kMaxTiles * kTile];
+    __shared__ double run_cos[kMode == kNearest ? kMaxTiles * kTile : kTile];   // the nearest of the groups before; kWeights: norms of the classes
+    __shared__ int run_c[kMode == kNearest ? kMaxTiles * kTile : 1];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, col = lane & 31, half = lane >> 5;
-    const int64_t all = (N + kTile - 1) / kTile, tile0 = (int64_t)blockIdx.x * tiles;
+    if constexpr (kMode == kWeights) {
+        const int idx = (int)blockIdx.x - ((int)gridDim.x - weigh.tblocks);
+        if (blockIdx.x == 0 && tid == 0 && weigh.reset) *weigh.reset = 0;
+        if (idx >= 0) {
+            static_assert(sizeof(TransposeTile) <= sizeof(sums), "the tile takes the sums' place");
+            transpose_tile<kThreads>(reinterpret_cast<TransposeTile &>(sums), idx, hv, N, W, weigh.G, weigh.colmask, weigh.ld, weigh.gw);
+            return;
+        }
+    }
+    const int64_t all = kMode == kWeights ? weigh.ld / kTile : (N + kTile - 1) / kTile, tile0 = (int64_t)blockIdx.x * tiles;
     const int count = (int)min((int64_t)tiles, all - tile0), parts = kParts ? (W + kBlocks - 1) / kBlocks : 1;
     const int g0 = blockIdx.y * groups, g1 = min(g0 + groups, (C + kTile - 1) / kTile);
 
@@ -209,10 +234,33 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     auto finish = [&](int g, int i, const double(&total)[2]) {
         const int c = g * kTile + c_of;
         const int64_t n = (tile0 + i) * kTile + n_of;
-        if constexpr (kPart) {
+        if constexpr (kMode == kDots) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
                 if (n < N && c + 16 * j < C) part[n * C + c + 16 * j] = total[j];
+        } else if constexpr (kMode == kWeights) {   // (as finish_cosines and online_weights_kernel, online_batched.hip)
+            const int y = n < N ? weigh.labels[n] : -1;
+            const bool live = y >= 0 && y < C;
+            Best best = {-2.0, kNoClass};   // cosines lie in [-1, 1]
+            double mine = 0.0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (c + 16 * j < C) {
+                    const double cs = size[j] == 0.0 ? 0.0 : total[j] / size[j];
+                    best = better(best, Best{cs, c + 16 * j});
+                    if (c + 16 * j == y) mine = cs;
+                }
+            best = best_of_16(best);
+            const double cos_y = sum_of_16(mine);
+            OnlineWeight r;
+            r.y = live ? y : -1;
+            r.pred = live && best.c != y ? best.c : -1;
+            r.w_y = live ? (float)(1.0 - cos_y) : 0.0f;
+            r.w_p = live ? (float)((double)weigh.lr * (1.0 - best.cos)) : 0.0f;
+            if (n < N && c_of == 0) weigh.records[n] = r;
+            if (weigh.coef)
+                for (int j = c_of; j < weigh.cb; j += 16)
+                    weigh.coef[n * weigh.cb + j] = j == r.y ? (double)r.w_y : j == r.pred ? -(double)r.w_p : 0.0;
         } else {
             Best best = {-__builtin_inf(), kNoClass};
 #pragma unroll
@@ -243,8 +291,19 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     ask(0, 0, word[0]);
     for (int g = g0; g < g1; ++g) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) size[j] = kPart ? 0.0 : norm[min(g * kTile + c_of + 16 * j, C - 1)];
+        for (int j = 0; j < 2; ++j) size[j] = kMode == kNearest ? norm[min(g * kTile + c_of + 16 * j, C - 1)] : 0.0;
+        if constexpr (kMode == kWeights) {   // sixteen lanes a class
+            double sum = 0.0;
+            for (int i = c_of; i < weigh.G; i += 16) sum += weigh.normpart[(int64_t)min(n_of, C - 1) * weigh.G + i];
+            sum = sum_of_16(sum);
+            if (c_of == 0) run_cos[n_of] = sum;
+        }
         if constexpr (!kParts) hold(g, 0);
+        if constexpr (kMode == kWeights) {
+            if constexpr (kParts) __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 2; ++j) size[j] = run_cos[c_of + 16 * j];
+        }
 #pragma unroll
         for (int j = 0; j < 2; ++j) size[j] = sqrt(size[j]) * root_d;
         if constexpr (!kParts) {
@@ -316,12 +375,12 @@ __global__ __launch_bounds__(256) void nearest_kernel(const double *__restrict__
     pred[n] = best.c == kNoClass ? 0 : best.c;
 }
 
-template <bool kPart>
+template <int kMode>
 void launch(hdc_ctx_impl *c, dim3 grid, hipStream_t s, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
-            int tiles, int groups, double *part, float *cos_out, int32_t *pred, double *best_cos, int *best_c) {
+            int tiles, int groups, double *part, float *cos_out, int32_t *pred, double *best_cos, int *best_c, const QuantWeights &weigh = {}) {
 #define HDC_SEARCH(STEPS, PARTS)                                                                                                                             \
-    hipLaunchKernelGGL((search_quantized_kernel<STEPS, PARTS, kPart>), grid, dim3(kThreads), 0, s, hv, N, c->W, c->p.C, codes, scales, norm, sqrt((double)c->p.D), \
-                       tiles, groups, part, cos_out, pred, best_cos, best_c)
+    hipLaunchKernelGGL((search_quantized_kernel<STEPS, PARTS, kMode>), grid, dim3(kThreads), 0, s, hv, N, c->W, c->p.C, codes, scales, norm, sqrt((double)c->p.D), \
+                       tiles, groups, part, cos_out, pred, best_cos, best_c, weigh)
     // Steps of a wave: as many as a row needs, up to 28 (the registers); rows of more than that go in parts of 16.
     const int steps = ((c->W + kWaves * 2 - 1) / (kWaves * 2) + 3) / 4 * 4;
     switch (steps) {
@@ -356,7 +415,7 @@ int launch_search_quantized(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, cons
     const int64_t blocks = (tiles + per - 1) / per, most = 1 << 22;   // blocks a launch
     for (int64_t b = 0; b < blocks; b += most) {
         const int64_t n0 = b * per * kTile, n = std::min(N - n0, most * per * kTile);
-        launch<false>(c, dim3((unsigned)std::min(most, blocks - b), (unsigned)splits), s, hv + n0 * c->W, n, codes, scales, norm, (int)per, of_split, nullptr,
+        launch<kNearest>(c, dim3((unsigned)std::min(most, blocks - b), (unsigned)splits), s, hv + n0 * c->W, n, codes, scales, norm, (int)per, of_split, nullptr,
                       cos_out ? cos_out + n0 * c->p.C : nullptr, splits > 1 ? nullptr : pred + n0, c->qs_cos_d, c->qs_class_d);
     }
     if (splits > 1)
@@ -371,8 +430,21 @@ int launch_quantized_dots(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const
     *slices = 1;
     const int64_t tiles = (nb + kTile - 1) / kTile, groups = (c->p.C + kTile - 1) / kTile;
     const int64_t per = std::max<int64_t>(1, (tiles * groups + c->num_cus - 1) / c->num_cus);
-    launch<true>(c, dim3((unsigned)((tiles + per - 1) / per), (unsigned)groups), s, hv, nb, codes, scales, nullptr, (int)per, 1, part, nullptr, nullptr, nullptr,
+    launch<kDots>(c, dim3((unsigned)((tiles + per - 1) / per), (unsigned)groups), s, hv, nb, codes, scales, nullptr, (int)per, 1, part, nullptr, nullptr, nullptr,
                  nullptr);
+    HDC_HIP(hipGetLastError());
+    return HDC_OK;
+}
+
+// Up to a group of classes, and up to as many samples as leave a block's work to a block.
+bool quantized_weights_takes(int C, int64_t nb) { return C <= kTile && nb <= 8192; }
+
+int launch_quantized_weights(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const uint32_t *codes, const uint8_t *scales, const QuantWeights &out,
+                             hipStream_t s) {
+    ProfScope prof(c, HDC_K_ONLINE_FWD, s);
+    const int64_t tiles = out.ld / kTile, per = std::max<int64_t>(1, (tiles + c->num_cus - 1) / c->num_cus);
+    launch<kWeights>(c, dim3((unsigned)((tiles + per - 1) / per + out.tblocks)), s, hv, nb, codes, scales, nullptr, (int)per, 1, nullptr, nullptr, nullptr,
+                     nullptr, nullptr, out);
     HDC_HIP(hipGetLastError());
     return HDC_OK;
 }

@@ -118,17 +118,21 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     constexpr int kAhead = !kParts && kSteps <= 20 ? 1 : 0;   // words of the next sample asked for before this one's products, or after them
     uint32_t word[1 + kAhead][kSteps];
 
-    // Step t has block 8 (t / 4) + 4 half + t % 4 of the wave's: a load of four words is 32 bytes of 32 rows.
-    // Words of sample tile i in part z of the row.  (Past the row's end, where the codes are zero, any word does.)
+    // A wave's blocks of part z are [w0, w0 + 2 kSteps), those before the row's end; it takes the row's last 2 kSteps where that is nearer, so
+    // that its loads need no limits, with codes of zero for the others'.  (Rows shorter than that: one by one, the last again.)
+    // Step t has block 8 (t / 4) + 4 half + t % 4 from there: a load of four words is 32 bytes of 32 rows.
+    const bool whole = W >= 2 * kSteps;
+    auto begin_of = [&](int z) { return min(z * kBlocks + wave * 2 * kSteps, W - 2 * kSteps); };
+    // Words of sample tile i in part z of the row.
     auto ask = [&](int i, int z, uint32_t(&to)[kSteps]) {
         const int64_t n = min((tile0 + i) * kTile + col, N - 1);
-        const int w0 = z * kBlocks + wave * 2 * kSteps;
         const uint32_t *const from = hv + n * W;
-        if (w0 + 2 * kSteps <= W) {
+        if (whole) {
+            const int w0 = begin_of(z) + 4 * half;
 #pragma unroll
-            for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&to[t], from + w0 + 2 * t + 4 * half, 16);
+            for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&to[t], from + w0 + 2 * t, 16);
         } else {
-            const int here = anew(w0 + 4 * half);   // (no places in the row are kept)
+            const int here = anew(wave * 2 * kSteps + 4 * half);   // (no places in the row are kept)
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) {
                 to[t] = from[min(here + 8 * (t / 4) + t % 4, W - 1)];
@@ -136,16 +140,28 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
             }
         }
     };
-    // This wave's codes of a group of classes in part z.  (Classes past the last are that one again.)
-    auto hold = [&](int group, int z) {
+    // This wave's codes of a group of classes in part z; meanwhile() is done while they are on their way.  (Classes past the last are that one
+    // again.)
+    auto hold = [&](int group, int z, auto meanwhile) {
         const int w0 = z * kBlocks + wave * 2 * kSteps;
         const int64_t from = anew((int64_t)min(group * kTile + col, C - 1) * W);
         const v4u *const here = reinterpret_cast<const v4u *>(codes) + from;
-        if (w0 + 2 * kSteps <= W) {
+        if (whole) {
+            const int begin = begin_of(z), first = begin + 4 * half;
 #pragma unroll
-            for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&scale[t / 4], scales + from + w0 + 2 * t + 4 * half, 4);
+            for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&scale[t / 4], scales + from + first + 2 * t, 4);
 #pragma unroll
-            for (int t = 0; t < kSteps; ++t) code[t] = here[w0 + 8 * (t / 4) + 4 * half + t % 4];
+            for (int t = 0; t < kSteps; ++t) code[t] = here[first + 8 * (t / 4) + t % 4];
+            if (begin < w0) {   // blocks before w0 are another wave's
+                const int place = anew(first);
+#pragma unroll
+                for (int t = 0; t < kSteps; ++t) {
+                    const bool mine = place + 8 * (t / 4) + t % 4 >= w0;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) code[t][r] = mine ? code[t][r] : 0u;
+                    scale[t / 4] &= mine ? ~0u : ~(255u << 8 * (t & 3));
+                }
+            }
         } else {
             const int begin = anew(w0 + 4 * half);
             uint32_t s[kSteps];
@@ -164,6 +180,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
                 for (int r = 0; r < 4; ++r) code[t][r] = in ? code[t][r] : 0u;
             }
         }
+        meanwhile();
         // Blocks of zeros, whose scale is 0 and may lie far from the others', count for nothing.
         uint32_t zeros = 0;
 #pragma unroll
@@ -288,19 +305,32 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         }
     };
 
+    constexpr int kEarly = kMode == kWeights ? 16 : 1;   // partial norms asked for first
+    double early[kEarly];
+    if constexpr (kMode == kWeights) {
+#pragma unroll
+        for (int i = 0; i < kEarly; ++i) early[i] = weigh.normpart[(int64_t)min(n_of, C - 1) * weigh.G + min(c_of + 16 * i, weigh.G - 1)];
+    }
     ask(0, 0, word[0]);
     for (int g = g0; g < g1; ++g) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) size[j] = kMode == kNearest ? norm[min(g * kTile + c_of + 16 * j, C - 1)] : 0.0;
-        if constexpr (kMode == kWeights) {   // sixteen lanes a class
-            double sum = 0.0;
-            for (int i = c_of; i < weigh.G; i += 16) sum += weigh.normpart[(int64_t)min(n_of, C - 1) * weigh.G + i];
-            sum = sum_of_16(sum);
-            if (c_of == 0) run_cos[n_of] = sum;
-        }
-        if constexpr (!kParts) hold(g, 0);
+        auto norms = [&]() {   // of the classes, sixteen lanes each
+            if constexpr (kMode == kWeights) {
+                double sum = 0.0;
+#pragma unroll
+                for (int i = 0; i < kEarly; ++i) sum += c_of + 16 * i < weigh.G ? early[i] : 0.0;
+                for (int i = c_of + 16 * kEarly; i < weigh.G; i += 16) sum += weigh.normpart[(int64_t)min(n_of, C - 1) * weigh.G + i];
+                sum = sum_of_16(sum);
+                if (c_of == 0) run_cos[n_of] = sum;
+            }
+        };
+        if constexpr (!kParts) hold(g, 0, norms);
         if constexpr (kMode == kWeights) {
-            if constexpr (kParts) __syncthreads();
+            if constexpr (kParts) {
+                norms();
+                __syncthreads();
+            }
 #pragma unroll
             for (int j = 0; j < 2; ++j) size[j] = run_cos[c_of + 16 * j];
         }
@@ -337,7 +367,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         for (int i = 0; i < count; ++i) {
             double total[2] = {0.0, 0.0};
             for (int z = 0; z < parts; ++z) {
-                if constexpr (kParts) hold(g, z);
+                if constexpr (kParts) hold(g, z, []() {});
                 double down = 1.0;
                 for (int p = 0; p < passes; ++p) {   // the blocks whose scale is one of this pass's: from 2^-(kRange + 1) p of the largest on downwards
                     v16f acc = {};

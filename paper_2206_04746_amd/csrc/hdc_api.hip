@@ -26,7 +26,7 @@ constexpr int64_t kPermRows = 1 << 22;       // rows grouped by class per traini
 static void free_ctx(hdc_ctx_impl *c) {
     if (!c) return;
     void *ptrs[] = {c->item_d, c->level_d, c->tie_d, c->lo_d, c->scale_d, c->q_d, c->cls_cnt_d,
-                    c->cls_off_d, c->cls_cur_d, c->cls_blk_d, c->perm_d, c->partial_d, c->qs_cos_d, c->qs_class_d, c->ob_part_d, c->ob_wts_d, c->ob_norm_d,
+                    c->cls_off_d, c->cls_cur_d, c->cls_blk_d, c->perm_d, c->partial_d, c->qs_cos_d, c->qs_class_d, c->qs_limits_d, c->ob_part_d, c->ob_wts_d, c->ob_norm_d,
                     c->ob_col_d, c->ob_carry_d, c->ob_coef_d, c->ob_share_d, c->on_bits_d, c->ob_ln_d, c->ob_lw_d, c->ob_meta_d,
                     c->oc_mem_d, c->os_mem_d,
                     c->citem_d, c->clevel_d, c->hvc_d, c->expand_d,
@@ -286,6 +286,7 @@ static int create(hdc_ctx **out, const hdc_params *p, const uint32_t *item, cons
     TRY(dev_alloc(&c->partial_d, (size_t)c->partial_items * c->Wp * 16));
     TRY(dev_alloc(&c->qs_cos_d, (size_t)search_quantized_entries(c)));
     TRY(dev_alloc(&c->qs_class_d, (size_t)search_quantized_entries(c)));
+    TRY(dev_alloc(&c->qs_limits_d, (size_t)search_many_limits()));
     TRY_HIP(hipDeviceSynchronize());
     try {
         TRY(prepare_compact(c, item, level, tie));

@@ -120,6 +120,7 @@ struct hdc_ctx_impl {
     // hdc_search_quantized: the nearest classes of groups of classes that different blocks search (quantized_search.hip).
     double *qs_cos_d;
     int *qs_class_d;
+    int *qs_limits_d;     // what the scales of the classes allow (quantized_many.hip)
 
     // hdc_encode_sparse (allocated and derived on its first call)
     bool sp_ready;
@@ -231,6 +232,11 @@ int launch_dequantize(hdc_ctx_impl *c, const uint32_t *codes, const uint8_t *sca
 int launch_search_quantized(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
                             float *cos_out, int32_t *pred, hipStream_t s);
 int64_t search_quantized_entries(const hdc_ctx_impl *c);   // of qs_cos_d and qs_class_d
+// Many samples and classes (quantized_many.hip); leaves the call to launch_search_quantized's own kernel if the scales of a row lie far apart.
+int64_t search_many_limits();   // of qs_limits_d
+bool search_many_takes(const hdc_ctx_impl *c, int64_t N);
+int launch_search_many(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm, float *cos_out,
+                       int32_t *pred, bool scan, int *splits, hipStream_t s);
 // Partial dot products [*slices][nb][C] of samples with the context's classes.
 int launch_quantized_dots(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const uint32_t *codes, const uint8_t *scales, double *part, int *slices,
                           hipStream_t s);

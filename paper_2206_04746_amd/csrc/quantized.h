@@ -27,6 +27,25 @@ __device__ __forceinline__ T anew(T v) {
     return v;
 }
 
+// Loads straight into LDS, 16 bytes a lane: lane i's go to `to` + 16 i.  By inline assembly, for a wave that has several on their way: around the
+// builtin the compiler waits for all of them before every read of LDS.  The kernel waits for them itself (all loads return in order; a
+// barrier alone does not wait), and keeps what it reads in between from places that are being loaded.
+struct LdsSource {
+    v4u words;   // a buffer's description
+};
+__device__ __forceinline__ LdsSource lds_source(const void *from, uint32_t bytes) {
+    const uint64_t at = reinterpret_cast<uint64_t>(from);
+    return {v4u{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32) & 0xFFFF),
+                (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u}};
+}
+__device__ __forceinline__ void load_lds(LdsSource from, uint32_t lane_offset, uint32_t offset, uint32_t *to) {
+    const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t *)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(at), "v"(lane_offset), "s"(from.words), "s"((uint32_t)__builtin_amdgcn_readfirstlane((int)offset))
+                 : "memory", "m0");
+}
+
 // 2^(s - 127) in 64 bits; a quiet NaN for a block that is no number.
 __device__ __forceinline__ double scale_value(int s) {
     return s == kQuantNone ? __longlong_as_double(0x7FF8000000000000ll) : __longlong_as_double((long long)(s + 896) << 52);

@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
                                                                        const double *__restrict__ norm, double root_d, int tiles, int groups,
                                                                        double *__restrict__ part, float *__restrict__ cos_out,
                                                                        int32_t *__restrict__ pred_out, double *__restrict__ best_cos, int *__restrict__ best_c,
-                                                                       QuantWeights weigh) {
+                                                                       QuantWeights weigh, const int *__restrict__ wide) {
     constexpr int kBlocks = kWaves * 2 * kSteps, kRange = range_of(kBlocks);   // of a row at a time
     constexpr int kPitch = kTile + 4;                                          // (sixteen classes by four samples lie in different banks)
     __shared__ float sums[2][kWaves][kTile][kPitch];
@@ -104,6 +104,13 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
             static_assert(sizeof(TransposeTile) <= sizeof(sums), "the tile takes the sums' place");
             transpose_tile<kThreads>(reinterpret_cast<TransposeTile &>(sums), idx, hv, N, W, weigh.G, weigh.colmask, weigh.ld, weigh.gw);
             return;
+        }
+    }
+    if constexpr (kMode == kNearest) {   // the call's other kernel has taken it, unless a row's scales lie far apart
+        if (wide) {
+            int any = 0;
+            for (int c = tid; c < C; c += kThreads) any |= wide[c];
+            if (!__syncthreads_or(any)) return;
         }
     }
     const int64_t all = kMode == kWeights ? weigh.ld / kTile : (N + kTile - 1) / kTile, tile0 = (int64_t)blockIdx.x * tiles;
@@ -407,10 +414,10 @@ __global__ __launch_bounds__(256) void nearest_kernel(const double *__restrict__
 
 template <int kMode>
 void launch(hdc_ctx_impl *c, dim3 grid, hipStream_t s, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
-            int tiles, int groups, double *part, float *cos_out, int32_t *pred, double *best_cos, int *best_c, const QuantWeights &weigh = {}) {
+            int tiles, int groups, double *part, float *cos_out, int32_t *pred, double *best_cos, int *best_c, const QuantWeights &weigh = {}, const int *wide = nullptr) {
 #define HDC_SEARCH(STEPS, PARTS)                                                                                                                             \
     hipLaunchKernelGGL((search_quantized_kernel<STEPS, PARTS, kMode>), grid, dim3(kThreads), 0, s, hv, N, c->W, c->p.C, codes, scales, norm, sqrt((double)c->p.D), \
-                       tiles, groups, part, cos_out, pred, best_cos, best_c, weigh)
+                       tiles, groups, part, cos_out, pred, best_cos, best_c, weigh, wide)
     // Steps of a wave: as many as a row needs, up to 28 (the registers); rows of more than that go in parts of 16.
     const int steps = ((c->W + kWaves * 2 - 1) / (kWaves * 2) + 3) / 4 * 4;
     switch (steps) {
@@ -428,30 +435,53 @@ void launch(hdc_ctx_impl *c, dim3 grid, hipStream_t s, const uint32_t *hv, int64
 
 }  // namespace
 
-// Entries of the scratch where the nearest classes of splits meet: a launch has splits only while its tiles leave compute units idle.
-int64_t search_quantized_entries(const hdc_ctx_impl *c) { return (int64_t)kTile * c->num_cus; }
+// Entries of the scratch where the nearest classes of splits meet: kTile samples a compute unit here, where a launch has splits only while
+// its tiles leave compute units idle; the other kernel takes as many samples at a time as there is room for.
+int64_t search_quantized_entries(const hdc_ctx_impl *c) { return std::max<int64_t>((int64_t)kTile * c->num_cus, 1 << 18); }
 
-int launch_search_quantized(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
-                            float *cos_out, int32_t *pred, hipStream_t s) {
-    ProfScope prof(c, HDC_K_SEARCH_QUANTIZED, s);
+static int launch_nearest(hdc_ctx_impl *c, int64_t N, int splits, int32_t *pred, hipStream_t s) {
+    hipLaunchKernelGGL(nearest_kernel, dim3((unsigned)((N + 255) / 256)), dim3(256), 0, s, c->qs_cos_d, c->qs_class_d, N, splits, pred);
+    HDC_HIP(hipGetLastError());
+    return HDC_OK;
+}
+
+// wide: null, or by class whether its scales lie far apart: if none's do, the call has been answered.
+static int launch_search_few(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
+                             float *cos_out, int32_t *pred, const int *wide, hipStream_t s) {
     const int groups = (c->p.C + kTile - 1) / kTile;
     const int64_t tiles = (N + kTile - 1) / kTile, cus = c->num_cus;
     // One block a compute unit.  One group of classes: as many tiles as that gives a block; more groups: the block walks over its tiles
     // for each, and where there are fewer tiles than compute units, the groups are split among blocks.
     int64_t per = std::max<int64_t>(1, (tiles + cus - 1) / cus);
     if (groups > 1) per = std::min<int64_t>(per, kMaxTiles);
-    const int splits_most = (int)std::max<int64_t>(1, std::min<int64_t>(groups, cus / tiles));
+    const int splits_most = wide ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(groups, cus / tiles));
     const int of_split = (groups + splits_most - 1) / splits_most, splits = (groups + of_split - 1) / of_split;
     const int64_t blocks = (tiles + per - 1) / per, most = 1 << 22;   // blocks a launch
     for (int64_t b = 0; b < blocks; b += most) {
         const int64_t n0 = b * per * kTile, n = std::min(N - n0, most * per * kTile);
         launch<kNearest>(c, dim3((unsigned)std::min(most, blocks - b), (unsigned)splits), s, hv + n0 * c->W, n, codes, scales, norm, (int)per, of_split, nullptr,
-                      cos_out ? cos_out + n0 * c->p.C : nullptr, splits > 1 ? nullptr : pred + n0, c->qs_cos_d, c->qs_class_d);
+                         cos_out ? cos_out + n0 * c->p.C : nullptr, splits > 1 ? nullptr : pred + n0, c->qs_cos_d, c->qs_class_d, {}, wide);
     }
-    if (splits > 1)
-        hipLaunchKernelGGL(nearest_kernel, dim3((unsigned)((N + 255) / 256)), dim3(256), 0, s, c->qs_cos_d, c->qs_class_d, N, splits, pred);
     HDC_HIP(hipGetLastError());
-    return HDC_OK;
+    return splits > 1 ? launch_nearest(c, N, splits, pred, s) : HDC_OK;
+}
+
+int launch_search_quantized(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
+                            float *cos_out, int32_t *pred, hipStream_t s) {
+    ProfScope prof(c, HDC_K_SEARCH_QUANTIZED, s);
+    if (search_many_takes(c, N)) {
+        const int64_t most = search_quantized_entries(c) / ((c->p.C + 127) / 128) / 256 * 256;   // samples at a time
+        for (int64_t n0 = 0; n0 < N; n0 += most) {
+            const int64_t n = std::min(most, N - n0);
+            float *const cos_of = cos_out ? cos_out + n0 * c->p.C : nullptr;
+            int splits = 1;
+            int rc = launch_search_many(c, hv + n0 * c->W, n, codes, scales, norm, cos_of, pred + n0, n0 == 0, &splits, s);
+            if (rc == HDC_OK && splits > 1) rc = launch_nearest(c, n, splits, pred + n0, s);
+            if (rc != HDC_OK) return rc;
+        }
+        return launch_search_few(c, hv, N, codes, scales, norm, cos_out, pred, c->qs_limits_d + search_many_limits() / 2, s);
+    }
+    return launch_search_few(c, hv, N, codes, scales, norm, cos_out, pred, nullptr, s);
 }
 
 int launch_quantized_dots(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const uint32_t *codes, const uint8_t *scales, double *part, int *slices,

@@ -197,6 +197,33 @@ def test_cosines_with_quantised_rows(N, C, D, kind):
     check_search(words(rng, N, D), x, want_cos=N % 2 == 1 or C < 7)
 
 
+# many samples and classes: tiles of 128 classes and 256 samples, with some past their ends
+MANY = [(16500, 65, 500), (8200, 129, 300), (9000, 200, 1021), (3000, 1000, 257), (2049, 1024, 2081), (33000, 64, 225)]
+
+
+@pytest.mark.parametrize("kind", ["normal", "zeros", "none", "orders"])
+@pytest.mark.parametrize("N,C,D", MANY)
+def test_cosines_of_many_samples_with_many_rows(N, C, D, kind):
+    rng = np.random.default_rng(N + C * 3 + D * 11)
+    x = rows_of("normal" if kind == "none" else kind, C, D, rng)
+    if kind == "none":
+        x[3, D // 2], x[C - 1, 0] = np.nan, np.inf
+    if kind == "zeros":
+        x[C // 2] = 0
+    check_search(words(rng, N, D), x, want_cos=N != 3000)
+
+
+@pytest.mark.parametrize("C", [70, 300])
+def test_equal_cosines_of_many_samples_go_to_the_lowest_class(C):
+    """Rows that repeat, within a tile of classes and across, and multiples of one another by powers of two."""
+    rng = np.random.default_rng(C)
+    N, D = 17000 if C == 70 else 8200, 400
+    x = rows_of("normal", C, D, rng)
+    x[9:] = x[rng.integers(0, 9, C - 9)] * np.exp2(rng.integers(-6, 7, C - 9))[:, None]
+    pred, want = check_search(words(rng, N, D), x.astype(np.float32))
+    assert np.all(pred < 9) and np.array_equal(pred, want[:, :9].argmax(1))
+
+
 def test_equal_cosines_go_to_the_lowest_class():
     """Rows that repeat, and rows that are multiples of one another by powers of two."""
     rng = np.random.default_rng(5)

@@ -92,20 +92,16 @@ constexpr int kScaleSteps = 2;                         // steps whose scales are
 // Blocks of 32 dimensions, `at` bytes into the rows, of kOf rows into LDS, a wave eight rows of 128 bytes at a time.  Rows past the last are
 // taken from it.
 template <int kOf>
-__device__ __forceinline__ void load_rows(const uint32_t *first, int rows, uint32_t pitch, uint32_t at, int wave, int lane, uint32_t *to) {
-    const auto from = __builtin_amdgcn_make_buffer_rsrc((void *)first, 0, (int)(rows * pitch), 0x00020000);
+__device__ __forceinline__ void load_rows(LdsSource from, int rows, uint32_t pitch, uint32_t at, int wave, int lane, uint32_t *to) {
     const int l = anew(lane) >> 3;   // (no address is kept through the products)
     if (rows == kOf) {
         const uint32_t mine = (uint32_t)l * pitch + at;
 #pragma unroll
-        for (int i = 0; i < kOf / 32; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)(to + (i * 32 + wave * 8) * kStep * 4), kUnit, (int)mine,
-                                                     (int)((i * 32 + wave * 8) * pitch), 0, 0);
+        for (int i = 0; i < kOf / 32; ++i) load_lds(from, mine, (uint32_t)(i * 32 + wave * 8) * pitch, to + (i * 32 + wave * 8) * kStep * 4);
     } else {
 #pragma unroll
         for (int i = 0; i < kOf / 32; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)(to + (i * 32 + wave * 8) * kStep * 4), kUnit,
-                                                     (int)((uint32_t)min(i * 32 + wave * 8 + l, rows - 1) * pitch + at), 0, 0, 0);
+            load_lds(from, (uint32_t)min(i * 32 + wave * 8 + l, rows - 1) * pitch + at, 0, to + (i * 32 + wave * 8) * kStep * 4);
     }
 }
 
@@ -144,11 +140,12 @@ __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_k
     const int rows_a = (int)min((int64_t)kRowsA, M - m0), rows_b = (int)min((int64_t)kRowsB, N - n0);
     const uint32_t pitch = (uint32_t)W * kUnit;
     const int steps = (W + kStep - 1) / kStep;
+    const LdsSource from_a = lds_source(a + m0 * W * 4, (uint32_t)rows_a * pitch), from_b = lds_source(b + n0 * W * 4, (uint32_t)rows_b * pitch);
 
     auto load = [&](int step) {   // (blocks past the row's end are taken from its last)
         const uint32_t at = (uint32_t)min(step * kStep + ((lane & 7) ^ ((wave & 1) * 4 + (lane >> 4))), W - 1) * kUnit;
-        load_rows<kRowsA>(a + m0 * W * 4, rows_a, pitch, at, wave, lane, unit[step & 1]);
-        load_rows<kRowsB>(b + n0 * W * 4, rows_b, pitch, at, wave, lane, unit[step & 1] + kRowsA * kStep * 4);
+        load_rows<kRowsA>(from_a, rows_a, pitch, at, wave, lane, unit[step & 1]);
+        load_rows<kRowsB>(from_b, rows_b, pitch, at, wave, lane, unit[step & 1] + kRowsA * kStep * 4);
     };
     uint32_t piece[kPieces][4];
     auto ask_scales = [&](int step) {
@@ -224,8 +221,8 @@ __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_k
         take(k, 2);
         multiply(std::integral_constant<int, 1>{});
         take(k, 3);
-        if (scales_too) put_scales(k + 1);
         multiply(std::integral_constant<int, 2>{});
+        if (scales_too) put_scales(k + 1);
         if (more) {
             meet(k + 1);
             if (k + 2 < steps) load(k + 2);

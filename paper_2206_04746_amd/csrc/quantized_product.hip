@@ -87,26 +87,9 @@ __global__ __launch_bounds__(kFewThreads) void product_few_kernel(const uint32_t
 
 // ---- many rows: a tile of 64 kA rows of a by 64 kB of b a block of two by two waves
 constexpr int kThreads = 256, kStep = 8, kUnit = 16;   // blocks of 32 dimensions a step, bytes of one
-constexpr int kScaleSteps = 2;                         // steps whose scales are asked for together
-
-// Blocks of 32 dimensions, `at` bytes into the rows, of kOf rows into LDS, a wave eight rows of 128 bytes at a time.  Rows past the last are
-// taken from it.
-template <int kOf>
-__device__ __forceinline__ void load_rows(LdsSource from, int rows, uint32_t pitch, uint32_t at, int wave, int lane, uint32_t *to) {
-    const int l = anew(lane) >> 3;   // (no address is kept through the products)
-    if (rows == kOf) {
-        const uint32_t mine = (uint32_t)l * pitch + at;
-#pragma unroll
-        for (int i = 0; i < kOf / 32; ++i) load_lds(from, mine, (uint32_t)(i * 32 + wave * 8) * pitch, to + (i * 32 + wave * 8) * kStep * 4);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kOf / 32; ++i)
-            load_lds(from, (uint32_t)min(i * 32 + wave * 8 + l, rows - 1) * pitch + at, 0, to + (i * 32 + wave * 8) * kStep * 4);
-    }
-}
 
 // The sums of a tile are computed here, and not past the next barrier: operands take the registers of those that have been multiplied.
-// (Sixteen tiles a wave are all of the accumulation registers.)
+// (Sixteen tiles a wave take all of the accumulation registers.)
 template <bool kAccumulators>
 __device__ __forceinline__ v16f settled(v16f v) {
     if constexpr (kAccumulators)
@@ -116,16 +99,20 @@ __device__ __forceinline__ v16f settled(v16f v) {
     return v;
 }
 
+// Steps of 256 dimensions.  While a step's matrix instructions are issued, four groups of kA kB, the operands of each next group are read
+// from LDS and, once all of the step's are in registers, the step after next is asked for in its place: all of it a piece to a
+// matrix instruction, so that these follow one another without a pause.  W >= kStep.
 template <int kA, int kB>
 __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
                                                                                       const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb,
                                                                                       int64_t N, int W, int tiles_m, int tiles_n, float *__restrict__ out) {
-    constexpr int kRowsA = 64 * kA, kRowsB = 64 * kB, kRows = kRowsA + kRowsB, kPieces = kRows / kThreads;   // of 16 bytes of scales
-    static_assert(kScaleSteps * kStep == 16, "a piece is a row's scales of these steps");
+    constexpr int kRowsA = 64 * kA, kRowsB = 64 * kB, kRows = kRowsA + kRowsB;
+    constexpr int kOwn = kRows / kThreads, kLoads = kRows / 32, kPer = kLoads / (kA * kB);   // rows whose scales a thread brings; loads of a step, and to a matrix instruction
+    static_assert(kLoads % (kA * kB) == 0 && kA + kB <= 2 * kA * kB, "pieces to a matrix instruction");
     // Codes of a step and of the next: block k of a row's eight is at place k ^ (row / 2 % 8) of the row, so that sixteen rows' blocks lie in
-    // different banks.
+    // different banks.  Scales of two steps and of the next two.
     __shared__ __align__(16) uint32_t unit[2][kRows * kStep * 4];
-    __shared__ uint32_t scale[2][kScaleSteps * kStep / 4][kRows];
+    __shared__ uint32_t scale[2][4][kRows];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
 
     // Blocks of consecutive numbers go to the eight dies in turn: a die takes tiles that lie together, eight rows of tiles wide.
@@ -142,99 +129,116 @@ __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_k
     const int steps = (W + kStep - 1) / kStep;
     const LdsSource from_a = lds_source(a + m0 * W * 4, (uint32_t)rows_a * pitch), from_b = lds_source(b + n0 * W * 4, (uint32_t)rows_b * pitch);
 
-    auto load = [&](int step) {   // (blocks past the row's end are taken from its last)
-        const uint32_t at = (uint32_t)min(step * kStep + ((lane & 7) ^ ((wave & 1) * 4 + (lane >> 4))), W - 1) * kUnit;
-        load_rows<kRowsA>(from_a, rows_a, pitch, at, wave, lane, unit[step & 1]);
-        load_rows<kRowsB>(from_b, rows_b, pitch, at, wave, lane, unit[step & 1] + kRowsA * kStep * 4);
+    // A step's blocks, or the row's last eight: those that the step before has had are zeros then.
+    auto begin_of = [&](int step) { return min(step * kStep, W - kStep); };
+    // A wave's load fills eight rows of 128 bytes; rows past the last are taken from it.
+    uint32_t offset[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int r = i * 32 + wave * 8 + (lane >> 3);
+        offset[i] = (uint32_t)(i * 32 < kRowsA ? min(r, rows_a - 1) : min(r - kRowsA, rows_b - 1)) * pitch + ((lane & 7) ^ ((wave & 1) * 4 + (lane >> 4))) * kUnit;
+    }
+    auto load = [&](int i, uint32_t *to, uint32_t begin) {
+        load_lds(i * 32 < kRowsA ? from_a : from_b, offset[i], begin * kUnit, to + (i * 32 + wave * 8) * kStep * 4);
     };
-    uint32_t piece[kPieces][4];
-    auto ask_scales = [&](int step) {
+    const uint8_t *own[kOwn];
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int r = anew(tid) + i * kThreads;
-            const uint8_t *const row = r < kRowsA ? sa + (m0 + min(r, rows_a - 1)) * W : sb + (n0 + min(r - kRowsA, rows_b - 1)) * W;
-            scale_bytes<16>(row, step * kStep, W, piece[i]);
-        }
+    for (int i = 0; i < kOwn; ++i) {
+        const int r = tid + i * kThreads;
+        own[i] = r < kRowsA ? sa + (m0 + min(r, rows_a - 1)) * W : sb + (n0 + min(r - kRowsA, rows_b - 1)) * W;
+    }
+    uint32_t piece[kOwn][4];
+    auto ask_scales = [&](int step) {   // of two steps
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) __builtin_memcpy(piece[i], own[i] + begin_of(step), 8), __builtin_memcpy(piece[i] + 2, own[i] + begin_of(step + 1), 8);
     };
-    auto put_scales = [&](int step) {
+    auto put_scales = [&](int to) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i)
+        for (int i = 0; i < kOwn; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) scale[step / kScaleSteps & 1][j][anew(tid) + i * kThreads] = piece[i][j];
+            for (int j = 0; j < 4; ++j) scale[to][j][tid + i * kThreads] = piece[i][j];
     };
 
     const int wm = (wave >> 1) * 32 * kA, wn = kRowsA + (wave & 1) * 32 * kB;   // this wave's rows
     v16f acc[kA][kB] = {};
-    v4u x[2][kA], y[2][kB];           // operands of a matrix instruction's dimensions, and of the next one's
+    v4u x[2][kA], y[2][kB];           // operands of a group of matrix instructions, and of the next
     uint32_t sx[2][kA], sy[2][kB];    // scales of a step, and of the next
-    auto take = [&](int step, int t) {
-        const uint32_t *const from = unit[step & 1] + (col * kStep + ((4 * half + t) ^ (col >> 1 & 7))) * 4;
-#pragma unroll
-        for (int i = 0; i < kA; ++i) x[t & 1][i] = *reinterpret_cast<const v4u *>(from + (wm + i * 32) * kStep * 4);
-#pragma unroll
-        for (int i = 0; i < kB; ++i) y[t & 1][i] = *reinterpret_cast<const v4u *>(from + (wn + i * 32) * kStep * 4);
+    const uint32_t *const codes_x = unit[0] + (wm + col) * kStep * 4, *const codes_y = unit[0] + (wn + col) * kStep * 4;
+    auto take = [&](int buffer, int t, int i) {   // the i-th operand of group t
+        const int place = buffer * kRows * kStep * 4 + ((4 * half + t) ^ (col >> 1 & 7)) * 4;
+        if (i < kA) x[t & 1][i] = *reinterpret_cast<const v4u *>(codes_x + place + i * 32 * kStep * 4);
+        else if (i < kA + kB) y[t & 1][i - kA] = *reinterpret_cast<const v4u *>(codes_y + place + (i - kA) * 32 * kStep * 4);
     };
-    auto take_scales = [&](int step, int to) {
-        const uint32_t *const from = scale[step / kScaleSteps & 1][step % kScaleSteps * 2 + half] + col;
+    auto take_scales = [&](int buffer, int step, int to) {
+        const uint32_t *const from = scale[buffer][step * 2 + half] + col;
 #pragma unroll
         for (int i = 0; i < kA; ++i) sx[to][i] = from[wm + i * 32];
 #pragma unroll
         for (int i = 0; i < kB; ++i) sy[to][i] = from[wn + i * 32];
     };
-    auto multiply = [&](auto t_of) {
+    // A group of matrix instructions, with meanwhile(i) after the i-th.
+    auto multiply = [&](auto t_of, int step, auto meanwhile) {
         constexpr int t = decltype(t_of)::value;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < kA; ++i)
 #pragma unroll
-            for (int j = 0; j < kB; ++j) acc[i][j] = mfma<t>(x[t & 1][i], y[t & 1][j], acc[i][j], sx[0][i], sy[0][j]);
+            for (int j = 0; j < kB; ++j) {
+                acc[i][j] = mfma<t>(x[t & 1][i], y[t & 1][j], acc[i][j], sx[step][i], sy[step][j]);
+                meanwhile(i * kB + j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
         for (int i = 0; i < kA; ++i)
 #pragma unroll
             for (int j = 0; j < kB; ++j) acc[i][j] = settled<(kA * kB > 8)>(acc[i][j]);
-        __builtin_amdgcn_sched_barrier(0);
     };
     // What a wave has asked for in LDS is there, for every wave, and what was there has been read by all.  (A barrier by itself does not wait for
     // loads into LDS.)
     auto meet = [&](int step) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (step * kStep + kStep > W) {   // blocks past the row's end: zeros
+        const int again = step * kStep - begin_of(step);   // blocks that the step before has had: of the last step, and past it
+        if (again > 0) {
             for (int u = tid; u < kRows * kStep; u += kThreads)
-                if (step * kStep + ((u & 7) ^ (u >> 4 & 7)) >= W) *reinterpret_cast<v4u *>(unit[step & 1] + u * 4) = v4u{0, 0, 0, 0};
+                if (((u & 7) ^ (u >> 4 & 7)) < again) *reinterpret_cast<v4u *>(unit[step & 1] + u * 4) = v4u{0, 0, 0, 0};
             __syncthreads();
         }
     };
+    // Step k, in buffer `odd`; what follows the row's last step is asked for and read as well, and not used.
+    auto go = [&](int k, auto odd_of) {
+        constexpr int odd = decltype(odd_of)::value;
+        const int chunk = k / 2 & 1;
+        if (!odd) ask_scales(k + 2);
+        multiply(std::integral_constant<int, 0>{}, odd, [&](int i) { take(odd, 1, i), i + kA * kB < kA + kB ? take(odd, 1, i + kA * kB) : (void)0; });
+        multiply(std::integral_constant<int, 1>{}, odd, [&](int i) { take(odd, 2, i), i + kA * kB < kA + kB ? take(odd, 2, i + kA * kB) : (void)0; });
+        multiply(std::integral_constant<int, 2>{}, odd, [&](int i) { take(odd, 3, i), i + kA * kB < kA + kB ? take(odd, 3, i + kA * kB) : (void)0; });
+        if (odd) put_scales(chunk ^ 1);
+        meet(k + 1);
+        const uint32_t begin = (uint32_t)begin_of(k + 2);
+        take_scales(odd ? chunk ^ 1 : chunk, odd ^ 1, odd ^ 1);
+        multiply(std::integral_constant<int, 3>{}, odd, [&](int i) {
+            take(odd ^ 1, 0, i), i + kA * kB < kA + kB ? take(odd ^ 1, 0, i + kA * kB) : (void)0;
+#pragma unroll
+            for (int l = 0; l < kPer; ++l) load(i * kPer + l, unit[odd], begin);
+        });
+    };
 
     ask_scales(0);
-    load(0);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(i, unit[0], (uint32_t)begin_of(0));
     put_scales(0);
     meet(0);
-    if (steps > 1) load(1);
-    take_scales(0, 0);
-    take(0, 0);
-    for (int k = 0; k < steps; ++k) {
-        const bool more = k + 1 < steps, scales_too = more && (k + 1) % kScaleSteps == 0;
-        if (scales_too) ask_scales(k + 1);
-        take(k, 1);
-        multiply(std::integral_constant<int, 0>{});
-        take(k, 2);
-        multiply(std::integral_constant<int, 1>{});
-        take(k, 3);
-        multiply(std::integral_constant<int, 2>{});
-        if (scales_too) put_scales(k + 1);
-        if (more) {
-            meet(k + 1);
-            if (k + 2 < steps) load(k + 2);
-            take_scales(k + 1, 1);
-            take(k + 1, 0);
-        }
-        multiply(std::integral_constant<int, 3>{});
 #pragma unroll
-        for (int i = 0; i < kA; ++i) sx[0][i] = sx[1][i];
+    for (int i = 0; i < kLoads; ++i) load(i, unit[1], (uint32_t)begin_of(1));
+    take_scales(0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < kB; ++i) sy[0][i] = sy[1][i];
+    for (int i = 0; i < kA + kB; ++i) take(0, 0, i);
+    for (int k = 0; k < steps; k += 2) {   // (a step past the last is one of zeros)
+        go(k, std::integral_constant<int, 0>{});
+        go(k + 1, std::integral_constant<int, 1>{});
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing may be on its way into LDS when the block's is given to another)
 #pragma unroll
     for (int i = 0; i < kA; ++i)
 #pragma unroll
@@ -257,7 +261,7 @@ int launch_product_quantized(hdc_ctx_impl *c, const uint32_t *a, const uint8_t *
     ProfScope prof(c, HDC_K_PRODUCT_QUANTIZED, s);
     const int W = c->W;
     const int64_t few = ((M + 31) / 32) * ((N + 31) / 32), large = ((M + 255) / 256) * ((N + 255) / 256), small = ((M + 127) / 128) * ((N + 127) / 128);
-    if (few < 4 * (int64_t)c->num_cus || N < 64 || M < 64) {
+    if (few < 4 * (int64_t)c->num_cus || N < 64 || M < 64 || W < kStep) {
         const int steps = ((W + 2 * kFewWaves - 1) / (2 * kFewWaves) + 3) / 4 * 4;
         for (int64_t m = 0; m < M; m += 32 * 65535) {
             const int64_t rows = std::min<int64_t>(M - m, 32 * 65535);

@@ -43,7 +43,7 @@ __device__ __forceinline__ void scale_bytes(const uint8_t *row, int at, int W, u
     }
 }
 
-// ---- few rows: 32 of a by 32 of b a block; the halves of a wave's lanes take steps of 32 dimensions from places of their own
+// ---- few rows: 32 of a by 32 of b a block; a wave's loads of four steps are the same lines of 32 rows of either side
 constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave;
 
 __global__ __launch_bounds__(kFewThreads) void product_few_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
@@ -54,19 +54,19 @@ __global__ __launch_bounds__(kFewThreads) void product_few_kernel(const uint32_t
     const int64_t m0 = (int64_t)blockIdx.y * kTile, n0 = (int64_t)blockIdx.x * kTile;
     const int64_t ra = min(m0 + col, M - 1) * W, rb = min(n0 + col, N - 1) * W;
     const v4u *const ca = reinterpret_cast<const v4u *>(a) + ra, *const cb = reinterpret_cast<const v4u *>(b) + rb;
-    const int first = (wave * 2 + half) * steps;   // steps: a multiple of 4
+    const int first = wave * 2 * steps + 4 * half;   // steps: a multiple of 4; step t has block 8 (t / 4) + 4 half + t % 4 of the wave's
     v16f acc = {};
     for (int t = 0; t < steps; t += 4) {
         v4u x[4], y[4];
         uint32_t sx[1], sy[1];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int w = first + t + i, in = min(w, W - 1);
+            const int w = first + 2 * t + i, in = min(w, W - 1);
             x[i] = ca[in], y[i] = cb[in];
             if (w >= W) x[i] = v4u{0, 0, 0, 0}, y[i] = v4u{0, 0, 0, 0};
         }
-        scale_bytes<4>(sa + ra, first + t, W, sx);
-        scale_bytes<4>(sb + rb, first + t, W, sy);
+        scale_bytes<4>(sa + ra, first + 2 * t, W, sx);
+        scale_bytes<4>(sb + rb, first + 2 * t, W, sy);
         acc = mfma<0>(x[0], y[0], acc, sx[0], sy[0]);
         acc = mfma<1>(x[1], y[1], acc, sx[0], sy[0]);
         acc = mfma<2>(x[2], y[2], acc, sx[0], sy[0]);
@@ -101,7 +101,7 @@ __device__ __forceinline__ v16f settled(v16f v) {
 
 // Steps of 256 dimensions.  While a step's matrix instructions are issued, four groups of kA kB, the operands of each next group are read
 // from LDS and, once all of the step's are in registers, the step after next is asked for in its place: all of it a piece to a
-// matrix instruction, so that these follow one another without a pause.  W >= kStep.
+// matrix instruction, so that these follow one another without a pause.  W >= 2 kStep.
 template <int kA, int kB>
 __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
                                                                                       const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb,
@@ -147,10 +147,12 @@ __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_k
         const int r = tid + i * kThreads;
         own[i] = r < kRowsA ? sa + (m0 + min(r, rows_a - 1)) * W : sb + (n0 + min(r - kRowsA, rows_b - 1)) * W;
     }
+    // The scales of two steps are sixteen bytes, or the row's last sixteen.
+    auto pair_of = [&](int step) { return min(step * kStep, W - 2 * kStep); };
     uint32_t piece[kOwn][4];
-    auto ask_scales = [&](int step) {   // of two steps
+    auto ask_scales = [&](int step) {
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) __builtin_memcpy(piece[i], own[i] + begin_of(step), 8), __builtin_memcpy(piece[i] + 2, own[i] + begin_of(step + 1), 8);
+        for (int i = 0; i < kOwn; ++i) __builtin_memcpy(piece[i], own[i] + pair_of(step), 16);
     };
     auto put_scales = [&](int to) {
 #pragma unroll
@@ -169,12 +171,19 @@ __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_k
         if (i < kA) x[t & 1][i] = *reinterpret_cast<const v4u *>(codes_x + place + i * 32 * kStep * 4);
         else if (i < kA + kB) y[t & 1][i - kA] = *reinterpret_cast<const v4u *>(codes_y + place + (i - kA) * 32 * kStep * 4);
     };
-    auto take_scales = [&](int buffer, int step, int to) {
-        const uint32_t *const from = scale[buffer][step * 2 + half] + col;
+    auto take_scales = [&](int step, int to) {
+        const int at = begin_of(step) - pair_of(step & ~1) + 4 * half;   // the first of this lane's four bytes among the sixteen
+        const uint32_t(*const from)[kRows] = &scale[step / 2 & 1][at >> 2];
 #pragma unroll
-        for (int i = 0; i < kA; ++i) sx[to][i] = from[wm + i * 32];
+        for (int i = 0; i < kA; ++i) sx[to][i] = from[0][wm + i * 32 + col];
 #pragma unroll
-        for (int i = 0; i < kB; ++i) sy[to][i] = from[wn + i * 32];
+        for (int i = 0; i < kB; ++i) sy[to][i] = from[0][wn + i * 32 + col];
+        if (at & 3) {   // (of the last steps, by the same for all lanes: the next word is one of the four)
+#pragma unroll
+            for (int i = 0; i < kA; ++i) sx[to][i] = __builtin_amdgcn_alignbyte(from[1][wm + i * 32 + col], sx[to][i], at & 3);
+#pragma unroll
+            for (int i = 0; i < kB; ++i) sy[to][i] = __builtin_amdgcn_alignbyte(from[1][wn + i * 32 + col], sy[to][i], at & 3);
+        }
     };
     // A group of matrix instructions, with meanwhile(i) after the i-th.
     auto multiply = [&](auto t_of, int step, auto meanwhile) {
@@ -216,7 +225,7 @@ __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_k
         if (odd) put_scales(chunk ^ 1);
         meet(k + 1);
         const uint32_t begin = (uint32_t)begin_of(k + 2);
-        take_scales(odd ? chunk ^ 1 : chunk, odd ^ 1, odd ^ 1);
+        take_scales(k + 1, odd ^ 1);
         multiply(std::integral_constant<int, 3>{}, odd, [&](int i) {
             take(odd ^ 1, 0, i), i + kA * kB < kA + kB ? take(odd ^ 1, 0, i + kA * kB) : (void)0;
 #pragma unroll
@@ -231,7 +240,7 @@ __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_k
     meet(0);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load(i, unit[1], (uint32_t)begin_of(1));
-    take_scales(0, 0, 0);
+    take_scales(0, 0);
 #pragma unroll
     for (int i = 0; i < kA + kB; ++i) take(0, 0, i);
     for (int k = 0; k < steps; k += 2) {   // (a step past the last is one of zeros)
@@ -261,14 +270,17 @@ int launch_product_quantized(hdc_ctx_impl *c, const uint32_t *a, const uint8_t *
     ProfScope prof(c, HDC_K_PRODUCT_QUANTIZED, s);
     const int W = c->W;
     const int64_t few = ((M + 31) / 32) * ((N + 31) / 32), large = ((M + 255) / 256) * ((N + 255) / 256), small = ((M + 127) / 128) * ((N + 127) / 128);
-    if (few < 4 * (int64_t)c->num_cus || N < 64 || M < 64 || W < kStep) {
+    // Few rows up to as many blocks as compute units, tiles of 128 rows up to two a unit, tiles of 256 beyond.  us, few / 128 / 256:
+    //   512 by 512 rows of 9999 24.6 26.8 64, of 4096 10.5 14.4 34; 1000 by 1000 of 9999 88 44 83, of 1000 14.2 8.7 20.7; 8192 by 1024 of 9999
+    //   685 73 89; 3000 by 3000 of 9999 885 109 91; 4096 by 4096 of 9999 1358 146 115, of 1000 174 25.1 24.9
+    if (few <= c->num_cus || W < 2 * kStep) {
         const int steps = ((W + 2 * kFewWaves - 1) / (2 * kFewWaves) + 3) / 4 * 4;
         for (int64_t m = 0; m < M; m += 32 * 65535) {
             const int64_t rows = std::min<int64_t>(M - m, 32 * 65535);
             hipLaunchKernelGGL(product_few_kernel, dim3((unsigned)((N + 31) / 32), (unsigned)((rows + 31) / 32)), dim3(kFewThreads), 0, s, a + m * W * 4,
                                sa + m * W, rows, b, sb, N, W, steps, out + m * N);
         }
-    } else if (large >= c->num_cus) {
+    } else if (small > 2 * (int64_t)c->num_cus) {
         hipLaunchKernelGGL((product_tiles_kernel<4, 4>), dim3((unsigned)large), dim3(kThreads), 0, s, a, sa, M, b, sb, N, W, (int)((M + 255) / 256),
                            (int)((N + 255) / 256), out);
     } else {

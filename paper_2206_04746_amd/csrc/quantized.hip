@@ -92,32 +92,59 @@ __global__ __launch_bounds__(1024) void quantize_rows_kernel(const float *__rest
     }
 }
 
-// Eight lanes a block, four adjacent dimensions a lane: nibble j of each of the block's words.
+// The four codes of dimensions 4 g to 4 g + 3 of a row, one a byte: nibble g & 7 of each of a block's words.
+__device__ __forceinline__ uint32_t four_codes(const uint32_t *__restrict__ codes, int64_t block, int g) {
+    const v4u word = *reinterpret_cast<const v4u *>(codes + block * 4);
+    uint32_t four = 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) four |= (word[r] >> 4 * (g & 7) & 15) << 8 * r;
+    return four;
+}
+
+constexpr int kLine = 32;   // floats of a cache line
+
+// Four floats a lane, so that a wave stores whole cache lines: in a row that starts `ahead` floats before sixteen aligned bytes these are
+// of two fours of codes, and the first lanes of a row, those before it in its first line, have nothing to do.  The stores leave the caches
+// alone.  Bound by memory: 6238 rows of 9999 (33 MB in, 249 MB out) take 47 us, 6.0 TB/s, where stores that follow the codes take 75 us,
+// those that also leave the caches alone 63; 60000 rows of 1001 take 59, for a line that two rows share is written twice.
 __global__ __launch_bounds__(256) void dequantize_rows_kernel(const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t N, int D,
                                                               int W, float *__restrict__ rows) {
-    const int tid = threadIdx.x, shift = 4 * (tid & 7);
-    for (int64_t n = blockIdx.y; n < N; n += gridDim.y)
-        for (int w = blockIdx.x * 32 + (tid >> 3); w < W; w += gridDim.x * 32) {
-            const int d = w * 32 + shift;
-            const v4u word = *reinterpret_cast<const v4u *>(codes + (n * W + w) * 4);
-            const int s = scales[n * W + w];
-            uint32_t four = 0, x[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) four |= (word[r] >> shift & 15) << 8 * r;
+    for (int64_t n = blockIdx.y; n < N; n += gridDim.y) {
+        float *const row = rows + n * D;
+        const int before = (int)((uintptr_t)row >> 2 & (kLine - 1)), ahead = -before & 3;   // uniform
+        for (int d = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 4 - before; d < D; d += gridDim.x * blockDim.x * 4) {
+            if (d <= -4) continue;
+            const int g = (d - ahead) >> 2;
+            uint32_t four = 0, next = 0;
+            int s = kQuantZero, t = kQuantZero;
+            if (g >= 0) {
+                const int64_t block = n * W + (g >> 3);
+                four = four_codes(codes, block, g);
+                s = scales[block];
+            }
+            if (ahead && 4 * g + 4 < D) {
+                const int64_t block = n * W + ((g + 1) >> 3);
+                next = four_codes(codes, block, g + 1);
+                t = scales[block];
+            }
+            four = __builtin_amdgcn_alignbyte(next, four, ahead);
             const uint32_t halves = __builtin_amdgcn_perm(0x0C080604u, 0x03020100u, four & 0x07070707u);
+            v4u x;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const uint32_t v = __float_as_uint(ldexpf((float)(halves >> 8 * r & 255), s - kQuantZero - 1));
-                x[r] = s == kQuantNone ? 0x7FC00000u : v | (four >> 8 * r & 8) << 28;
+                const int scale = r + ahead < 4 ? s : t;
+                const uint32_t v = __float_as_uint(ldexpf((float)(halves >> 8 * r & 255), scale - kQuantZero - 1));
+                x[r] = scale == kQuantNone ? 0x7FC00000u : v | (four >> 8 * r & 8) << 28;
             }
-            if (d + 4 <= D) {
-                __builtin_memcpy(rows + n * D + d, x, 16);
+            if (d >= 0 && d + 4 <= D) {
+                __builtin_nontemporal_store(x, reinterpret_cast<v4u *>(row + d));
             } else {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (d + r < D) rows[n * D + d + r] = __uint_as_float(x[r]);
+                    if (d + r >= 0 && d + r < D) row[d + r] = __uint_as_float(x[r]);
             }
         }
+    }
 }
 
 }  // namespace
@@ -136,9 +163,12 @@ int launch_quantize(hdc_ctx_impl *c, const float *rows, int64_t N, uint32_t *cod
 }
 
 int launch_dequantize(hdc_ctx_impl *c, const uint32_t *codes, const uint8_t *scales, int64_t N, float *rows, hipStream_t s) {
-    const int64_t chunks = (c->W + 31) / 32;
-    const dim3 grid((unsigned)std::min(chunks, std::max<int64_t>(1, 64 * (int64_t)c->num_cus / N)), (unsigned)std::min<int64_t>(N, 65535));
-    hipLaunchKernelGGL(dequantize_rows_kernel, grid, dim3(256), 0, s, codes, scales, N, c->p.D, c->W, rows);
+    // A wave writes 1 KiB at a time, twice where there are rows enough (6238 rows of 9999: once 57 us, twice 47, three times 56, five times 48;
+    // 60000 of 1000: 46, 41, 45 and 50).
+    const int64_t steps = (c->p.D + kLine - 1 + 255) / 256, each = N * steps >= 128 * (int64_t)c->num_cus ? 2 : 1;
+    const int64_t waves = (steps + each - 1) / each, chunks = (waves + 3) / 4;
+    hipLaunchKernelGGL(dequantize_rows_kernel, dim3((unsigned)chunks, (unsigned)std::min<int64_t>(N, 65535)),
+                       dim3((unsigned)std::min<int64_t>(waves, 4) * kWave), 0, s, codes, scales, N, c->p.D, c->W, rows);
     HDC_HIP(hipGetLastError());
     return HDC_OK;
 }

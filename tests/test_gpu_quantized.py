@@ -131,6 +131,27 @@ def test_neighbours_of_the_rows_are_left_alone():
     ctx.close()
 
 
+@pytest.mark.parametrize("D", [1, 3, 29, 64, 257, 1000, 2055])
+def test_rows_written_from_any_place(D):
+    """Rows that start anywhere in a cache line, with blocks that are no numbers and the bits beyond D set; what is around them is left alone."""
+    rng = np.random.default_rng(D)
+    N, W = 41, (D + 31) // 32
+    codes = rng.integers(0, 2 ** 32, size=(N, 4 * W), dtype=np.uint32)
+    scales = rng.choice(np.array([0, 1, 100, 127, 128, 140, 252, 255], np.uint8), size=(N, W))
+    with np.errstate(over="ignore"):
+        want = oq.values(codes, scales, D).astype(np.float32)
+    ctx = context(D)
+    c, s = dev_u32(codes), torch.from_numpy(scales).cuda()
+    for start in (0, 1, 2, 3, 4, 5, 7, 12, 30, 31, 33):
+        room = torch.full((start + N * D + 40,), 9.0, device="cuda")
+        ctx.hdc_dequantize(c, s, room[start:start + N * D].view(N, D))
+        torch.cuda.synchronize()
+        got = room.cpu().numpy()
+        assert same_bits(got[start:start + N * D].reshape(N, D), want)
+        assert np.all(got[:start] == 9) and np.all(got[start + N * D:] == 9)
+    ctx.close()
+
+
 def test_scales_that_quantisation_does_not_give():
     """s = 253 and 254: values beyond fp32 are infinite; every code at every scale."""
     D = 512

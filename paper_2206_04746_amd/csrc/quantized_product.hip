@@ -3,7 +3,8 @@
 //
 // Many rows: tiles of a's rows by b's rows through LDS, 256 dimensions at a time (128 bytes a row, loaded straight into LDS), the next step's
 // while a step's are multiplied; within a step a wave takes the operands of its next matrix instructions while it issues these.
-// Few rows: a block takes 32 by 32 rows, its waves a part of the dimensions each, without LDS but for the sum over the waves.
+// Few rows: a block takes 32 by 32 rows, or 16 by 16 (v_mfma_scale_f32_16x16x128_f8f6f4), its waves a share of the dimensions each, without LDS
+// but for the sum over the waves.
 #include <algorithm>
 #include <type_traits>
 
@@ -43,45 +44,64 @@ __device__ __forceinline__ void scale_bytes(const uint8_t *row, int at, int W, u
     }
 }
 
-// ---- few rows: 32 of a by 32 of b a block; a wave's loads of four steps are the same lines of 32 rows of either side
-constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave;
+// ---- few rows: kSize of a by kSize of b a block, 32 or 16, a share of the dimensions to each of its waves
+constexpr int kFewWaves = 8;
 
-__global__ __launch_bounds__(kFewThreads) void product_few_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
-                                                                  const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb, int64_t N, int W,
-                                                                  int steps, float *__restrict__ out) {
-    __shared__ float sums[kFewWaves][kTile][kTile + 1];
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, col = lane & 31, half = lane >> 5;
-    const int64_t m0 = (int64_t)blockIdx.y * kTile, n0 = (int64_t)blockIdx.x * kTile;
+template <int kSize>
+struct FewSums;
+template <>
+struct FewSums<32> {
+    typedef v16f type;
+};
+template <>
+struct FewSums<16> {
+    typedef float type __attribute__((ext_vector_type(4)));
+};
+
+template <int B>
+__device__ __forceinline__ FewSums<16>::type mfma(v4u a, v4u b, FewSums<16>::type c, uint32_t sa, uint32_t sb) {
+    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, B, (int)sa, B, (int)sb);
+}
+
+// A wave takes the blocks of 32 dimensions of four matrix instructions at a time, four adjacent ones a lane, and then those that are as many
+// further on as the waves have.  Bound by the latency of its loads, 64 bytes of a row each.
+template <int kSize>
+__global__ __launch_bounds__(kFewWaves * kWave) void product_few_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
+                                                                        const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb, int64_t N, int W,
+                                                                        float *__restrict__ out) {
+    constexpr int kGroups = kWave / kSize, kPerUnit = 4 * kGroups;   // lanes to a row, blocks of four instructions
+    __shared__ float sums[kFewWaves][kSize][kSize + 1];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, waves = blockDim.x >> 6, col = lane % kSize, group = lane / kSize;
+    const int64_t m0 = (int64_t)blockIdx.y * kSize, n0 = (int64_t)blockIdx.x * kSize;
     const int64_t ra = min(m0 + col, M - 1) * W, rb = min(n0 + col, N - 1) * W;
     const v4u *const ca = reinterpret_cast<const v4u *>(a) + ra, *const cb = reinterpret_cast<const v4u *>(b) + rb;
-    const int first = wave * 2 * steps + 4 * half;   // steps: a multiple of 4; step t has block 8 (t / 4) + 4 half + t % 4 of the wave's
-    v16f acc = {};
-    for (int t = 0; t < steps; t += 4) {
+    typename FewSums<kSize>::type acc = {};
+    for (int u = wave * kPerUnit; u < W; u += waves * kPerUnit) {   // uniform
+        const int first = u + 4 * group;
         v4u x[4], y[4];
         uint32_t sx[1], sy[1];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int w = first + 2 * t + i, in = min(w, W - 1);
+            const int w = first + i, in = min(w, W - 1);
             x[i] = ca[in], y[i] = cb[in];
             if (w >= W) x[i] = v4u{0, 0, 0, 0}, y[i] = v4u{0, 0, 0, 0};
         }
-        scale_bytes<4>(sa + ra, first + 2 * t, W, sx);
-        scale_bytes<4>(sb + rb, first + 2 * t, W, sy);
+        scale_bytes<4>(sa + ra, first, W, sx);
+        scale_bytes<4>(sb + rb, first, W, sy);
         acc = mfma<0>(x[0], y[0], acc, sx[0], sy[0]);
         acc = mfma<1>(x[1], y[1], acc, sx[0], sy[0]);
         acc = mfma<2>(x[2], y[2], acc, sx[0], sy[0]);
         acc = mfma<3>(x[3], y[3], acc, sx[0], sy[0]);
     }
 #pragma unroll
-    for (int j = 0; j < 16; ++j) sums[wave][8 * (j / 4) + 4 * half + j % 4][col] = acc[j];
+    for (int j = 0; j < kSize * kSize / kWave; ++j) sums[wave][4 * kGroups * (j / 4) + 4 * group + j % 4][col] = acc[j];
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int r = (tid >> 5) + 16 * j;
-        double sum = 0.0;   // of eight fp32 sums, rounded once
-#pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) sum += (double)sums[w][r][col];
-        if (m0 + r < M && n0 + col < N) out[(m0 + r) * N + n0 + col] = (float)sum;
+    for (int at = tid; at < kSize * kSize; at += blockDim.x) {
+        const int r = at / kSize, k = at % kSize;
+        double sum = 0.0;   // of the waves' fp32 sums, rounded once
+        for (int w = 0; w < waves; ++w) sum += (double)sums[w][r][k];
+        if (m0 + r < M && n0 + k < N) out[(m0 + r) * N + n0 + k] = (float)sum;
     }
 }
 
@@ -269,17 +289,25 @@ int launch_product_quantized(hdc_ctx_impl *c, const uint32_t *a, const uint8_t *
                              hipStream_t s) {
     ProfScope prof(c, HDC_K_PRODUCT_QUANTIZED, s);
     const int W = c->W;
-    const int64_t few = ((M + 31) / 32) * ((N + 31) / 32), large = ((M + 255) / 256) * ((N + 255) / 256), small = ((M + 127) / 128) * ((N + 127) / 128);
-    // Few rows up to as many blocks as compute units, tiles of 128 rows up to two a unit, tiles of 256 beyond.  us, few / 128 / 256:
-    //   512 by 512 rows of 9999 24.6 26.8 64, of 4096 10.5 14.4 34; 1000 by 1000 of 9999 88 44 83, of 1000 14.2 8.7 20.7; 8192 by 1024 of 9999
-    //   685 73 89; 3000 by 3000 of 9999 885 109 91; 4096 by 4096 of 9999 1358 146 115, of 1000 174 25.1 24.9
+    const int64_t fewest = ((M + 15) / 16) * ((N + 15) / 16), few = ((M + 31) / 32) * ((N + 31) / 32), large = ((M + 255) / 256) * ((N + 255) / 256), small = ((M + 127) / 128) * ((N + 127) / 128);
+    // Few rows up to as many blocks as compute units, in 16 by 16 up to as many blocks of these; tiles of 128 rows up to two a unit, tiles of
+    // 256 beyond.  us a call, 16 by 16 / 32 by 32: 64 by 64 rows of 9999 6.6 9.9, 1559 by 26 6.8 9.8 (196 blocks of 16 by 16); 96 by 1000 14.2
+    // 10.5 (378), 512 by 512 21 13.5, of 16384 40 23.  us, few / 128 / 256: 512 by 512 rows of 9999 13.5 26.8 64; 1000 by 1000 of 9999 88 44 83,
+    // of 1000 14.2 8.7 20.7; 8192 by 1024 of 9999 685 73 89; 3000 by 3000 of 9999 885 109 91; 4096 by 4096 of 9999 1358 146 115, of 1000
+    // 174 25.1 24.9.
     if (few <= c->num_cus || W < 2 * kStep) {
-        const int steps = ((W + 2 * kFewWaves - 1) / (2 * kFewWaves) + 3) / 4 * 4;
-        for (int64_t m = 0; m < M; m += 32 * 65535) {
-            const int64_t rows = std::min<int64_t>(M - m, 32 * 65535);
-            hipLaunchKernelGGL(product_few_kernel, dim3((unsigned)((N + 31) / 32), (unsigned)((rows + 31) / 32)), dim3(kFewThreads), 0, s, a + m * W * 4,
-                               sa + m * W, rows, b, sb, N, W, steps, out + m * N);
-        }
+        auto launch = [&](auto kernel, int size) {
+            const int per = 4 * kWave / size, waves = std::min((W + per - 1) / per, kFewWaves);
+            for (int64_t m = 0; m < M; m += (int64_t)size * 65535) {
+                const int64_t rows = std::min<int64_t>(M - m, (int64_t)size * 65535);
+                hipLaunchKernelGGL(kernel, dim3((unsigned)((N + size - 1) / size), (unsigned)((rows + size - 1) / size)), dim3((unsigned)waves * kWave), 0, s,
+                                   a + m * W * 4, sa + m * W, rows, b, sb, N, W, out + m * N);
+            }
+        };
+        if (fewest <= c->num_cus)
+            launch(product_few_kernel<16>, 16);
+        else
+            launch(product_few_kernel<32>, 32);
     } else if (small > 2 * (int64_t)c->num_cus) {
         hipLaunchKernelGGL((product_tiles_kernel<4, 4>), dim3((unsigned)large), dim3(kThreads), 0, s, a, sa, M, b, sb, N, W, (int)((M + 255) / 256),
                            (int)((N + 255) / 256), out);

@@ -288,7 +288,7 @@ def check_product(xa, xb):
 
 
 PRODUCT = [(1, 1, 1), (1, 26, 10000), (26, 1, 10000), (2, 3, 31), (16, 16, 128), (17, 15, 129), (32, 33, 64), (33, 31, 65), (100, 26, 500), (64, 130, 1000),
-           (129, 257, 777), (300, 200, 3001), (1, 1000, 1024), (700, 2, 4097), (5, 7, 70001), (255, 513, 96)]
+           (129, 257, 777), (300, 200, 3001), (1, 1000, 1024), (700, 2, 4097), (5, 7, 70001), (255, 513, 96), (400, 300, 3001)]
 
 
 @pytest.mark.parametrize("kind", ["normal", "orders", "zeros", "tiny"])

@@ -1,7 +1,7 @@
 // Cosine inference with class rows of 4-bit floats (arXiv 2206.04746, Sec. III), and the dot products of online training with them.
 //
 // The matrix cores take such rows as they are, with their scales (v_mfma_scale_f32_32x32x64_f8f6f4), and a sample's bits as +-1 in the
-// same format.  A block of eight waves takes 32 classes and walks over the samples, 32 at a time; each wave has an eighth of the
+// same format.  A block of eight waves takes 32 classes, or the model's up to 16, and walks over the samples, 32 at a time; each wave has an eighth of the
 // dimensions and holds the codes of its classes there in registers, so that all there is to read on the way is the samples, once.
 // The waves' parts of the dot products meet in LDS.
 //
@@ -19,11 +19,12 @@ namespace hdc {
 
 namespace {
 
-constexpr int kWaves = 8, kThreads = kWaves * kWave, kTile = 32;   // classes, samples
+constexpr int kWaves = 8, kThreads = kWaves * kWave, kTile = 32;   // samples; most classes of a block
 constexpr int kMaxTiles = 32;                                      // of samples a block walks over once for every group of classes
 constexpr int kNoClass = 0x7FFFFFFF;
 
 typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
 // The largest difference of scales of so many blocks.
@@ -37,6 +38,11 @@ template <int B>
 __device__ __forceinline__ v16f mfma(v4u a, v4u b, v16f c, uint32_t scale) {
     const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, B, (int)scale, 0, 0x7F7F7F7F);
+}
+template <int B>
+__device__ __forceinline__ v4f mfma(v4u a, v4u b, v4f c, uint32_t scale) {
+    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, B, (int)scale, 0, 0x7F7F7F7F);
 }
 
 // +-1 of a word's 32 dimensions in the order of the codes: 2 is the code of 1, 10 that of -1.
@@ -83,20 +89,22 @@ __device__ __forceinline__ double sum_of_16(double v) {
 //   kDots     part[n][C] takes the dot products
 //   kWeights  up to 32 classes: the weights of online training (`weigh`); the last weigh.tblocks blocks transpose the samples' bits
 enum Mode { kNearest, kDots, kWeights };
-template <int kSteps, bool kParts, int kMode>
+template <int kClasses, int kSteps, bool kParts, int kMode>
 __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uint32_t *__restrict__ hv, int64_t N, int W, int C,
                                                                        const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                                        const double *__restrict__ norm, double root_d, int tiles, int groups,
                                                                        double *__restrict__ part, float *__restrict__ cos_out,
                                                                        int32_t *__restrict__ pred_out, double *__restrict__ best_cos, int *__restrict__ best_c,
                                                                        QuantWeights weigh, const int *__restrict__ wide) {
-    constexpr int kBlocks = kWaves * 2 * kSteps, kRange = range_of(kBlocks);   // of a row at a time
+    constexpr int kPieces = kWave / kClasses, kCols = kTile / kClasses, kOwn = kClasses / 16;   // lanes to a row; rows of samples to a lane; classes of a thread
+    constexpr int kBlocks = kWaves * kPieces * kSteps, kRange = range_of(kBlocks);              // of a row at a time
+    typedef typename std::conditional<kClasses == 32, v16f, v4f>::type Sums;
     constexpr int kPitch = kTile + 4;                                          // (sixteen classes by four samples lie in different banks)
     __shared__ float sums[2][kWaves][kTile][kPitch];
     __shared__ int limits[2][kWaves][kTile];                    // largest and smallest scale of a class in a wave's dimensions
     __shared__ double run_cos[kMode == kNearest ? kMaxTiles * kTile : kTile];   // the nearest of the groups before; kWeights: norms of the classes
     __shared__ int run_c[kMode == kNearest ? kMaxTiles * kTile : 1];
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, col = lane % kClasses, piece = lane / kClasses;
     if constexpr (kMode == kWeights) {
         const int idx = (int)blockIdx.x - ((int)gridDim.x - weigh.tblocks);
         if (blockIdx.x == 0 && tid == 0 && weigh.reset) *weigh.reset = 0;
@@ -115,73 +123,76 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     }
     const int64_t all = kMode == kWeights ? weigh.ld / kTile : (N + kTile - 1) / kTile, tile0 = (int64_t)blockIdx.x * tiles;
     const int count = (int)min((int64_t)tiles, all - tile0), parts = kParts ? (W + kBlocks - 1) / kBlocks : 1;
-    const int g0 = blockIdx.y * groups, g1 = min(g0 + groups, (C + kTile - 1) / kTile);
+    const int g0 = blockIdx.y * groups, g1 = min(g0 + groups, (C + kClasses - 1) / kClasses);
 
     v4u code[kSteps];
     uint32_t scale[kSteps / 4];   // a byte a step, less `top` (modulo 2^32, all four together): 127 for the row's largest
     int top = 0, passes = 1;      // the row's largest scale less 127; passes that the block needs
-    double unit[2], size[2];      // of this thread's two classes: the largest scale, the row's norm times that of a sample
+    double unit[kOwn], size[kOwn];   // of this thread's classes: the largest scale, the row's norm times that of a sample
     const int n_of = tid >> 4, c_of = tid & 15;   // this thread's sample of a tile, and the first of its classes, which are 16 apart
     constexpr int kAhead = !kParts && kSteps <= 20 ? 1 : 0;   // words of the next sample asked for before this one's products, or after them
-    uint32_t word[1 + kAhead][kSteps];
+    uint32_t word[1 + kAhead][kCols][kSteps];
 
-    // A wave's blocks of part z are [w0, w0 + 2 kSteps), those before the row's end; it takes the row's last 2 kSteps where that is nearer, so
+    // A wave's blocks of part z are [w0, w0 + kPieces kSteps), those before the row's end; it takes the row's last ones where that is nearer, so
     // that its loads need no limits, with codes of zero for the others'.  (Rows shorter than that: one by one, the last again.)
-    // Step t has block 8 (t / 4) + 4 half + t % 4 from there: a load of four words is 32 bytes of 32 rows.
-    const bool whole = W >= 2 * kSteps;
-    auto begin_of = [&](int z) { return min(z * kBlocks + wave * 2 * kSteps, W - 2 * kSteps); };
+    // Step t has block kPieces (t & ~3) + 4 piece + t % 4 from there: a load of four words is 16 kPieces bytes of kClasses rows.
+    const bool whole = W >= kPieces * kSteps;
+    auto begin_of = [&](int z) { return min(z * kBlocks + wave * kPieces * kSteps, W - kPieces * kSteps); };
     // Words of sample tile i in part z of the row.
-    auto ask = [&](int i, int z, uint32_t(&to)[kSteps]) {
-        const int64_t n = min((tile0 + i) * kTile + col, N - 1);
-        const uint32_t *const from = hv + n * W;
-        if (whole) {
-            const int w0 = begin_of(z) + 4 * half;
+    auto ask = [&](int i, int z, uint32_t(&to)[kCols][kSteps]) {
 #pragma unroll
-            for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&to[t], from + w0 + 2 * t, 16);
-        } else {
-            const int here = anew(wave * 2 * kSteps + 4 * half);   // (no places in the row are kept)
+        for (int k = 0; k < kCols; ++k) {
+            const int64_t n = min((tile0 + i) * kTile + kClasses * k + col, N - 1);
+            const uint32_t *const from = hv + n * W;
+            if (whole) {
+                const int w0 = begin_of(z) + 4 * piece;
 #pragma unroll
-            for (int t = 0; t < kSteps; ++t) {
-                to[t] = from[min(here + 8 * (t / 4) + t % 4, W - 1)];
-                if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (not all addresses at once)
+                for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&to[k][t], from + w0 + kPieces * t, 16);
+            } else {
+                const int here = anew(wave * kPieces * kSteps + 4 * piece);   // (no places in the row are kept)
+#pragma unroll
+                for (int t = 0; t < kSteps; ++t) {
+                    to[k][t] = from[min(here + kPieces * (t & ~3) + t % 4, W - 1)];
+                    if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (not all addresses at once)
+                }
             }
         }
     };
     // This wave's codes of a group of classes in part z; meanwhile() is done while they are on their way.  (Classes past the last are that one
     // again.)
     auto hold = [&](int group, int z, auto meanwhile) {
-        const int w0 = z * kBlocks + wave * 2 * kSteps;
-        const int64_t from = anew((int64_t)min(group * kTile + col, C - 1) * W);
+        const int w0 = z * kBlocks + wave * kPieces * kSteps;
+        const int64_t from = anew((int64_t)min(group * kClasses + col, C - 1) * W);
         const v4u *const here = reinterpret_cast<const v4u *>(codes) + from;
         if (whole) {
-            const int begin = begin_of(z), first = begin + 4 * half;
+            const int begin = begin_of(z), first = begin + 4 * piece;
 #pragma unroll
-            for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&scale[t / 4], scales + from + first + 2 * t, 4);
+            for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&scale[t / 4], scales + from + first + kPieces * t, 4);
 #pragma unroll
-            for (int t = 0; t < kSteps; ++t) code[t] = here[first + 8 * (t / 4) + t % 4];
+            for (int t = 0; t < kSteps; ++t) code[t] = here[first + kPieces * (t & ~3) + t % 4];
             if (begin < w0) {   // blocks before w0 are another wave's
                 const int place = anew(first);
 #pragma unroll
                 for (int t = 0; t < kSteps; ++t) {
-                    const bool mine = place + 8 * (t / 4) + t % 4 >= w0;
+                    const bool mine = place + kPieces * (t & ~3) + t % 4 >= w0;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) code[t][r] = mine ? code[t][r] : 0u;
                     scale[t / 4] &= mine ? ~0u : ~(255u << 8 * (t & 3));
                 }
             }
         } else {
-            const int begin = anew(w0 + 4 * half);
+            const int begin = anew(w0 + 4 * piece);
             uint32_t s[kSteps];
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) {
-                const int w = min(begin + 8 * (t / 4) + t % 4, W - 1);
+                const int w = min(begin + kPieces * (t & ~3) + t % 4, W - 1);
                 s[t] = scales[from + w];
                 code[t] = here[w];
                 if (t % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (not all addresses at once)
             }
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) {
-                const bool in = begin + 8 * (t / 4) + t % 4 < W;
+                const bool in = begin + kPieces * (t & ~3) + t % 4 < W;
                 scale[t / 4] = (t % 4 ? scale[t / 4] : 0u) | (in ? s[t] : 0u) << 8 * (t % 4);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) code[t][r] = in ? code[t][r] : 0u;
@@ -205,15 +216,18 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
             most = max(most, zeros >> t & 1 ? -1 : s);
             least = min(least, zeros >> t & 1 ? 256 : s);
         }
-        most = max(most, __shfl_xor(most, 32, kWave));
-        least = min(least, __shfl_xor(least, 32, kWave));
+#pragma unroll
+        for (int off = kClasses; off < kWave; off <<= 1) {
+            most = max(most, __shfl_xor(most, off, kWave));
+            least = min(least, __shfl_xor(least, off, kWave));
+        }
         __syncthreads();   // what is written here has been read
-        if (half == 0) limits[0][wave][col] = most, limits[1][wave][col] = least;
+        if (piece == 0) limits[0][wave][col] = most, limits[1][wave][col] = least;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) most = max(most, limits[0][w][col]), least = min(least, limits[1][w][col]);
         passes = most < 0 || most == kQuantNone ? 1 : (most - least) / (kRange + 1) + 1;   // (of a row that is no number, any)
-        for (int off = 1; off < 32; off <<= 1) passes = max(passes, __shfl_xor(passes, off, kWave));
+        for (int off = 1; off < kClasses; off <<= 1) passes = max(passes, __shfl_xor(passes, off, kWave));
         passes = __builtin_amdgcn_readfirstlane(passes);
         if (__ballot(zeros != 0) != 0) {   // blocks of zeros as the largest
 #pragma unroll
@@ -223,7 +237,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
 #pragma unroll
         for (int t = 0; t < kSteps; t += 4) scale[t / 4] -= 0x01010101u * (uint32_t)top;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < kOwn; ++j) {
             int largest = -1;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) largest = max(largest, limits[0][w][c_of + 16 * j]);
@@ -232,22 +246,28 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     };
 
     // This wave's part of a tile's dot products, where the codes need one pass.
-    auto multiply = [&]() {
-        v16f acc = {};
+    auto multiply = [&](Sums(&acc)[kCols]) {
+#pragma unroll
+        for (int k = 0; k < kCols; ++k) acc[k] = Sums{};
 #pragma unroll
         for (int t = 0; t < kSteps; t += 4) {
-            acc = mfma<0>(code[t], signs_of(word[0][t]), acc, scale[t / 4]);
-            acc = mfma<1>(code[t + 1], signs_of(word[0][t + 1]), acc, scale[t / 4]);
-            acc = mfma<2>(code[t + 2], signs_of(word[0][t + 2]), acc, scale[t / 4]);
-            acc = mfma<3>(code[t + 3], signs_of(word[0][t + 3]), acc, scale[t / 4]);
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) {
+                acc[k] = mfma<0>(code[t], signs_of(word[0][k][t]), acc[k], scale[t / 4]);
+                acc[k] = mfma<1>(code[t + 1], signs_of(word[0][k][t + 1]), acc[k], scale[t / 4]);
+                acc[k] = mfma<2>(code[t + 2], signs_of(word[0][k][t + 2]), acc[k], scale[t / 4]);
+                acc[k] = mfma<3>(code[t + 3], signs_of(word[0][k][t + 3]), acc[k], scale[t / 4]);
+            }
             __builtin_amdgcn_sched_barrier(0);   // (not all signs at once: their registers)
         }
-        return acc;
     };
-    auto put = [&](int turn, v16f acc) {
+    auto put = [&](int turn, const Sums(&acc)[kCols]) {
         float(*const to)[kPitch] = sums[turn][wave];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) to[8 * (j / 4) + 4 * half + j % 4][col] = acc[j];
+        for (int k = 0; k < kCols; ++k) {
+#pragma unroll
+            for (int j = 0; j < kClasses * kClasses / kWave; ++j) to[4 * kPieces * (j / 4) + 4 * piece + j % 4][kClasses * k + col] = acc[k][j];
+        }
     };
     auto sum_of = [&](int turn, int j) {
         float sum = 0.0f;   // without rounding
@@ -255,12 +275,12 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         for (int w = 0; w < kWaves; ++w) sum += sums[turn][w][c_of + 16 * j][n_of];
         return sum;
     };
-    auto finish = [&](int g, int i, const double(&total)[2]) {
-        const int c = g * kTile + c_of;
+    auto finish = [&](int g, int i, const double(&total)[kOwn]) {
+        const int c = g * kClasses + c_of;
         const int64_t n = (tile0 + i) * kTile + n_of;
         if constexpr (kMode == kDots) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < kOwn; ++j)
                 if (n < N && c + 16 * j < C) part[n * C + c + 16 * j] = total[j];
         } else if constexpr (kMode == kWeights) {   // (as finish_cosines and online_weights_kernel, online_batched.hip)
             const int y = n < N ? weigh.labels[n] : -1;
@@ -268,7 +288,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
             Best best = {-2.0, kNoClass};   // cosines lie in [-1, 1]
             double mine = 0.0;
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < kOwn; ++j)
                 if (c + 16 * j < C) {
                     const double cs = size[j] == 0.0 ? 0.0 : total[j] / size[j];
                     best = better(best, Best{cs, c + 16 * j});
@@ -288,7 +308,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         } else {
             Best best = {-__builtin_inf(), kNoClass};
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < kOwn; ++j)
                 if (c + 16 * j < C) {
                     const double cs = size[j] == 0.0 ? 0.0 : total[j] / size[j];
                     if (cos_out && n < N) cos_out[n * C + c + 16 * j] = (float)cs;
@@ -321,7 +341,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     ask(0, 0, word[0]);
     for (int g = g0; g < g1; ++g) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) size[j] = kMode == kNearest ? norm[min(g * kTile + c_of + 16 * j, C - 1)] : 0.0;
+        for (int j = 0; j < kOwn; ++j) size[j] = kMode == kNearest ? norm[min(g * kClasses + c_of + 16 * j, C - 1)] : 0.0;
         auto norms = [&]() {   // of the classes, sixteen lanes each
             if constexpr (kMode == kWeights) {
                 double sum = 0.0;
@@ -339,10 +359,10 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
                 __syncthreads();
             }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) size[j] = run_cos[c_of + 16 * j];
+            for (int j = 0; j < kOwn; ++j) size[j] = run_cos[c_of + 16 * j];
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) size[j] = sqrt(size[j]) * root_d;
+        for (int j = 0; j < kOwn; ++j) size[j] = sqrt(size[j]) * root_d;
         if constexpr (!kParts) {
             if (__builtin_expect(passes == 1, 1)) {
                 // A tile is finished while the next one's products are formed, by half of the waves before and by the other half after their own:
@@ -350,16 +370,23 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
                 const int one = anew(1);   // (no loop of its own for the first tile)
                 for (int i = 0; i <= count; ++i) {
                     auto before = [&]() {
-                        const double total[2] = {(double)sum_of((i - 1) & 1, 0) * unit[0], (double)sum_of((i - 1) & 1, 1) * unit[1]};
+                        double total[kOwn];
+#pragma unroll
+                        for (int j = 0; j < kOwn; ++j) total[j] = (double)sum_of((i - 1) & 1, j) * unit[j];
                         finish(g, i - 1, total);
                     };
                     if (i >= one && wave < kWaves / 2) before();
                     if (i < count) {
                         if constexpr (kAhead) ask(i + 1 < count ? i + 1 : 0, 0, word[kAhead]);
-                        put(i & 1, multiply());
+                        Sums acc[kCols];
+                        multiply(acc);
+                        put(i & 1, acc);
                         if constexpr (kAhead) {
 #pragma unroll
-                            for (int t = 0; t < kSteps; ++t) word[0][t] = word[kAhead][t];
+                            for (int k = 0; k < kCols; ++k) {
+#pragma unroll
+                                for (int t = 0; t < kSteps; ++t) word[0][k][t] = word[kAhead][k][t];
+                            }
                         } else {
                             ask(i + 1 < count ? i + 1 : 0, 0, word[0]);
                         }
@@ -372,26 +399,30 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         }
         int turn = 0;
         for (int i = 0; i < count; ++i) {
-            double total[2] = {0.0, 0.0};
+            double total[kOwn] = {};
             for (int z = 0; z < parts; ++z) {
                 if constexpr (kParts) hold(g, z, []() {});
                 double down = 1.0;
                 for (int p = 0; p < passes; ++p) {   // the blocks whose scale is one of this pass's: from 2^-(kRange + 1) p of the largest on downwards
-                    v16f acc = {};
+                    Sums acc[kCols] = {};
 #pragma unroll
-                    for (int t = 0; t < kSteps; ++t) word[0][t] = anew(word[0][t]);   // (or all signs would be made before the loop)
+                    for (int k = 0; k < kCols; ++k) {   // (or all signs would be made before the loop)
+#pragma unroll
+                        for (int t = 0; t < kSteps; ++t) word[0][k][t] = anew(word[0][k][t]);
+                    }
                     top = anew(top);
 #pragma unroll
                     for (int t = 0; t < kSteps; ++t) {
                         const int of = (int)((scale[t / 4] + 0x01010101u * (uint32_t)top) >> 8 * (t & 3) & 255) - top + (kRange + 1) * p;
                         const uint32_t mine = of <= kQuantZero && of >= kQuantZero - kRange ? ~0u : 0u;
-                        acc = mfma<0>(code[t] & mine, signs_of(word[0][t]), acc, (uint32_t)of & mine);
+#pragma unroll
+                        for (int k = 0; k < kCols; ++k) acc[k] = mfma<0>(code[t] & mine, signs_of(word[0][k][t]), acc[k], (uint32_t)of & mine);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                     put(turn, acc);
                     __syncthreads();
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) total[j] = fma((double)sum_of(turn, j), unit[j] * down, total[j]);
+                    for (int j = 0; j < kOwn; ++j) total[j] = fma((double)sum_of(turn, j), unit[j] * down, total[j]);
                     turn ^= 1;
                     down *= 1.0 / (2 << kRange);
                 }
@@ -412,23 +443,38 @@ __global__ __launch_bounds__(256) void nearest_kernel(const double *__restrict__
     pred[n] = best.c == kNoClass ? 0 : best.c;
 }
 
+// Classes of a block: for no more than 16 (v_mfma_scale_f32_16x16x128_f8f6f4) half of the loads and registers (2947 samples of 10000 with 6
+// classes 6.9 us a call, in a block for 32 7.7; a batch of 64 in training 8.5 us, 8.9).
+int quantized_classes(const hdc_ctx_impl *c) { return c->p.C > 16 ? 32 : 16; }
+
 template <int kMode>
 void launch(hdc_ctx_impl *c, dim3 grid, hipStream_t s, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
             int tiles, int groups, double *part, float *cos_out, int32_t *pred, double *best_cos, int *best_c, const QuantWeights &weigh = {}, const int *wide = nullptr) {
-#define HDC_SEARCH(STEPS, PARTS)                                                                                                                             \
-    hipLaunchKernelGGL((search_quantized_kernel<STEPS, PARTS, kMode>), grid, dim3(kThreads), 0, s, hv, N, c->W, c->p.C, codes, scales, norm, sqrt((double)c->p.D), \
-                       tiles, groups, part, cos_out, pred, best_cos, best_c, weigh, wide)
-    // Steps of a wave: as many as a row needs, up to 28 (the registers); rows of more than that go in parts of 16.
-    const int steps = ((c->W + kWaves * 2 - 1) / (kWaves * 2) + 3) / 4 * 4;
-    switch (steps) {
-        case 4: HDC_SEARCH(4, false); break;
-        case 8: HDC_SEARCH(8, false); break;
-        case 12: HDC_SEARCH(12, false); break;
-        case 16: HDC_SEARCH(16, false); break;
-        case 20: HDC_SEARCH(20, false); break;
-        case 24: HDC_SEARCH(24, false); break;
-        case 28: HDC_SEARCH(28, false); break;
-        default: HDC_SEARCH(16, true); break;
+#define HDC_SEARCH(CLASSES, STEPS, PARTS)                                                                                                             \
+    hipLaunchKernelGGL((search_quantized_kernel<CLASSES, STEPS, PARTS, kMode>), grid, dim3(kThreads), 0, s, hv, N, c->W, c->p.C, codes, scales, norm, \
+                       sqrt((double)c->p.D), tiles, groups, part, cos_out, pred, best_cos, best_c, weigh, wide)
+    // Steps of a wave: as many as a row needs, up to 20 or 28 (the registers); rows of more than that go in parts of 16.
+    const int classes = quantized_classes(c), blocks = kWaves * (kWave / classes), steps = ((c->W + blocks - 1) / blocks + 3) / 4 * 4;
+    if (classes == 16) {
+        switch (steps) {
+            case 4: HDC_SEARCH(16, 4, false); break;
+            case 8: HDC_SEARCH(16, 8, false); break;
+            case 12: HDC_SEARCH(16, 12, false); break;
+            case 16: HDC_SEARCH(16, 16, false); break;
+            case 20: HDC_SEARCH(16, 20, false); break;
+            default: HDC_SEARCH(16, 16, true); break;
+        }
+    } else {
+        switch (steps) {
+            case 4: HDC_SEARCH(32, 4, false); break;
+            case 8: HDC_SEARCH(32, 8, false); break;
+            case 12: HDC_SEARCH(32, 12, false); break;
+            case 16: HDC_SEARCH(32, 16, false); break;
+            case 20: HDC_SEARCH(32, 20, false); break;
+            case 24: HDC_SEARCH(32, 24, false); break;
+            case 28: HDC_SEARCH(32, 28, false); break;
+            default: HDC_SEARCH(32, 16, true); break;
+        }
     }
 #undef HDC_SEARCH
 }

@@ -1059,7 +1059,7 @@ static int train_pieces(hdc_ctx_impl *c, const uint32_t *hv, const int32_t *labe
                 const QuantWeights out = {labels + b0 + s0, c->ob_norm_d, static_cast<OnlineWeight *>(c->ob_wts_d), cb && !lists ? c->ob_coef_d : nullptr,
                                           c->ob_col_d, lists ? c->ob_meta_d + 3 * C : nullptr, ld_used, lr, G, cb,
                                           lists ? kListGroups : bwd_shares(c, G, nb) > 1 ? bwd_group_width(C) : 1, tblocks};
-                if (quant && quantized_weights_takes(C, nb)) {
+                if (quant && quantized_weights_takes(C)) {
                     rc = launch_quantized_weights(c, rows, nb, quant->codes, quant->scales, out, s);
                     if (rc != HDC_OK) return rc;
                 } else {

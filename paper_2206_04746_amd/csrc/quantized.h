@@ -85,7 +85,7 @@ struct QuantWeights {
     float lr;
     int G, cb, gw, tblocks;   // blocks for the transposed bits
 };
-bool quantized_weights_takes(int C, int64_t nb);
+bool quantized_weights_takes(int C);
 int launch_quantized_weights(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const uint32_t *codes, const uint8_t *scales, const QuantWeights &out,
                              hipStream_t s);
 

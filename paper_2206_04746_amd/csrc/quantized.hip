@@ -152,9 +152,10 @@ __global__ __launch_bounds__(256) void dequantize_rows_kernel(const uint32_t *__
 // Rows beyond a launch's 65535 are taken by the same blocks.
 int launch_quantize(hdc_ctx_impl *c, const float *rows, int64_t N, uint32_t *codes, uint8_t *scales, double *norm, double *part, hipStream_t s) {
     ProfScope prof(c, HDC_K_QUANTIZE_ROWS, s);
-    // A wave to 512 dimensions, a block of up to sixteen waves to a row: four where there are rows enough for every compute unit's.
-    // Without norms to be summed over the row, several blocks where there are few rows.
-    const int steps = (c->W + 15) / 16, waves = std::min(steps, N >= 8 * (int64_t)c->num_cus ? 4 : norm ? 16 : 4);
+    // A wave takes 512 dimensions at a time, a block of up to four waves a row; up to sixteen where there are fewer rows than compute units
+    // (a row of 100000: 14 us a call, with four 31; 2000 rows of 9999: 21, with four 17).  Without norms to be summed over a row, several
+    // blocks of four where there are few rows instead (a row of 100000 6.5 us, in one block 30; 6238 rows of 9999 46, in one 44).
+    const int steps = (c->W + 15) / 16, waves = std::min(steps, norm && N < (int64_t)c->num_cus ? 16 : 4);
     const int chunks = norm ? 1 : (int)std::min<int64_t>((steps + waves - 1) / waves, std::max<int64_t>(1, 8 * (int64_t)c->num_cus / N));
     hipLaunchKernelGGL(quantize_rows_kernel, dim3((unsigned)chunks, (unsigned)std::min<int64_t>(N, 65535)), dim3((unsigned)waves * kWave), 0, s, rows, N,
                        c->p.D, c->W, codes, scales, norm, part, (c->p.D + kWave - 1) / kWave);

@@ -283,10 +283,13 @@ int range_of(int blocks) {
 
 int64_t search_many_limits() { return 2 * kMost; }
 
-// Whether a call goes this way, unless its rows' scales lie far apart.
+// Whether a call goes this way, unless its rows' scales lie far apart: where the classes fill more than half of a block's and there are blocks
+// for three of eight compute units.  us, so and by search_quantized_kernel; classes by samples of 10000 dimensions: 64 by 64000 (250 blocks)
+// 72 49, 96 71 72, 128 74 93; 128 by 16000 (63) 62 43; 256 by 4000 (32) 61 36, by 16000 (126) 65 80; 1024 by 4000 (128) 70 123, by 64000 381
+// 652.  Of 1000: 64 by 64000 29 26, 96 29 39, 128 by 16000 19 23, 1024 by 1000 (32) 24 22, by 16000 35 152.
 bool search_many_takes(const hdc_ctx_impl *c, int64_t N) {
-    return c->p.C >= 64 && c->W >= kStep && (int64_t)c->W * kUnit * kClasses < ((int64_t)1 << 31) &&
-           (N + kSamples - 1) / kSamples * ((c->p.C + kClasses - 1) / kClasses) >= c->num_cus / 2;
+    return c->p.C > kClasses / 2 && c->W >= kStep && (int64_t)c->W * kUnit * kClasses < ((int64_t)1 << 31) &&
+           (N + kSamples - 1) / kSamples * ((c->p.C + kClasses - 1) / kClasses) >= c->num_cus * 3 / 8;
 }
 
 // One launch for samples that the scratch of the nearest classes has room for; *splits: classes' tiles, 1 if pred is written already.

@@ -219,7 +219,8 @@ def test_cosines_with_quantised_rows(N, C, D, kind):
 
 
 # many samples and classes: tiles of 128 classes and 256 samples, with some past their ends
-MANY = [(16500, 65, 500), (8200, 129, 300), (9000, 200, 1021), (3000, 1000, 257), (2049, 1024, 2081), (33000, 64, 225)]
+MANY = [(16500, 65, 500), (8200, 129, 300), (9000, 200, 1021), (3000, 1000, 257), (2049, 1024, 2081), (33000, 64, 225),
+        (25000, 65, 500), (12545, 129, 300), (13000, 200, 1021), (3100, 1024, 2081), (24577, 128, 4097), (33000, 1024, 290)]
 
 
 @pytest.mark.parametrize("kind", ["normal", "zeros", "none", "orders"])
@@ -234,11 +235,11 @@ def test_cosines_of_many_samples_with_many_rows(N, C, D, kind):
     check_search(words(rng, N, D), x, want_cos=N != 3000)
 
 
-@pytest.mark.parametrize("C", [70, 300])
-def test_equal_cosines_of_many_samples_go_to_the_lowest_class(C):
+@pytest.mark.parametrize("N,C", [(17000, 70), (25000, 70), (8200, 300)])
+def test_equal_cosines_of_many_samples_go_to_the_lowest_class(N, C):
     """Rows that repeat, within a tile of classes and across, and multiples of one another by powers of two."""
     rng = np.random.default_rng(C)
-    N, D = 17000 if C == 70 else 8200, 400
+    D = 400
     x = rows_of("normal", C, D, rng)
     x[9:] = x[rng.integers(0, 9, C - 9)] * np.exp2(rng.integers(-6, 7, C - 9))[:, None]
     pred, want = check_search(words(rng, N, D), x.astype(np.float32))
@@ -350,7 +351,7 @@ def run_training(hv, y, acc, batch, epochs, lr, reserve=True):
     return rows.cpu().numpy(), codes.cpu().numpy().view(np.uint32), scales.cpu().numpy(), norm.cpu().numpy()
 
 
-TRAIN = [(1, 1, 1), (3, 2, 31), (40, 5, 100), (64, 6, 1024), (100, 26, 500), (33, 40, 300), (1500, 20, 200), (2100, 6, 130), (500, 300, 96), (7, 3, 10000)]
+TRAIN = [(1, 1, 1), (3, 2, 31), (40, 5, 100), (64, 6, 1024), (100, 26, 500), (33, 40, 300), (1500, 20, 200), (2100, 6, 130), (500, 300, 96), (7, 3, 10000), (20000, 6, 130), (20000, 26, 97)]
 
 
 @pytest.mark.parametrize("start", ["zeros", "sums"])

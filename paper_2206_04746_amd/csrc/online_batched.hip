@@ -366,7 +366,6 @@ __global__ __launch_bounds__(256, 8) void online_weights_kernel(
 typedef const uint64_t __attribute__((address_space(4))) *kptr_u64;
 typedef const double __attribute__((address_space(4))) *kptr_f64;
 
-//
 // kQuant: the rows are answered with in 4 bits (hdc_train_online_quantized): on the last launch of a batch the elements are quantised as they
 // are updated, and normpart takes the squared norm of what they have become.
 template <int CB, bool kQuant>

@@ -14,6 +14,53 @@ constexpr int kQuantNone = 255;   // the scale of a block that is no number
 constexpr int kQuantZero = 127;   // the scale byte of 1
 
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+// Products of 32 rows by 32 over 64 dimensions, or 16 by 16 over 128, on the matrix cores: a lane has the codes of a block of a row of either
+// side, its scales in byte B of a register.
+template <int BA, int BB>
+__device__ __forceinline__ v16f mfma_codes(v4u a, v4u b, v16f c, uint32_t sa, uint32_t sb) {
+    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, BA, (int)sa, BB, (int)sb);
+}
+template <int BA, int BB>
+__device__ __forceinline__ v4f mfma_codes(v4u a, v4u b, v4f c, uint32_t sa, uint32_t sb) {
+    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, BA, (int)sa, BB, (int)sb);
+}
+template <int B, typename Sums>
+__device__ __forceinline__ Sums mfma(v4u a, v4u b, Sums c, uint32_t sa, uint32_t sb) {
+    return mfma_codes<B, B>(a, b, c, sa, sb);
+}
+template <int B, typename Sums>   // with samples, whose scale is 1
+__device__ __forceinline__ Sums mfma(v4u a, v4u b, Sums c, uint32_t sa) {
+    return mfma_codes<B, 0>(a, b, c, sa, 0x7F7F7F7Fu);
+}
+
+// +-1 of a word's 32 dimensions in the order of the codes: 2 is the code of 1, 10 that of -1.
+__device__ __forceinline__ v4u signs_of(uint32_t word) {
+    v4u out;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) out[r] = ((word << (3 - r)) & 0x88888888u) ^ 0xAAAAAAAAu;
+    return out;
+}
+
+// The largest difference of scales of so many blocks whose sums with samples are without rounding in fp32.
+constexpr int range_of(int blocks) {
+    int r = 0;
+    while ((int64_t)blocks * 192 * 2 << (r + 1) <= 1 << 24) ++r;
+    return r;
+}
+
+// The nearest class so far; of equals the lowest.
+constexpr int kNoClass = 0x7FFFFFFF;
+struct Best {
+    double cos;
+    int c;
+};
+__device__ __forceinline__ Best better(Best a, Best b) { return b.cos > a.cos || (b.cos == a.cos && b.c < a.c) ? b : a; }
 
 // Magnitude of a code in halves.
 __device__ __forceinline__ int code_halves(uint32_t code) { return (int)(0x0C08060403020100ull >> 8 * (code & 7) & 255); }

@@ -20,17 +20,7 @@ constexpr int kA = 4, kB = 2;                        // tiles of classes of a wa
 constexpr int kClasses = kA * kTile, kSamples = kWaves * kB * kTile;
 constexpr int kStep = 8, kUnit = 16;                 // blocks of 32 dimensions a step, bytes of one's codes
 constexpr int kBuffers = 3;                          // steps in LDS
-constexpr int kNoClass = 0x7FFFFFFF;
 
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef float v16f __attribute__((ext_vector_type(16)));
-typedef float v4f __attribute__((ext_vector_type(4)));
-
-template <int B>
-__device__ __forceinline__ v16f mfma(v4u a, v4u b, v16f c, uint32_t scale) {
-    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, B, (int)scale, 0, 0x7F7F7F7F);
-}
 
 // limits[c]: the largest scale of row c (-1: a row of zeros); limits[kMost + c]: whether its scales lie further apart than 2^range.
 constexpr int kMost = HDC_MAX_C;
@@ -57,12 +47,6 @@ __global__ __launch_bounds__(256) void scan_kernel(const uint32_t *__restrict__ 
         limits[kMost + c] = most >= 0 && most != kQuantNone && most - least > range;
     }
 }
-
-struct Best {
-    double cos;
-    int c;
-};
-__device__ __forceinline__ Best better(Best a, Best b) { return b.cos > a.cos || (b.cos == a.cos && b.c < a.c) ? b : a; }
 
 // grid: classes' tiles of eight samples' tiles at a time, a die's together.  pred_out, or best_cos and best_c [classes' tile][N].
 __global__ __launch_bounds__(kThreads, 2) void search_many_kernel(const uint32_t *__restrict__ hv, int64_t N, int W, int C,
@@ -157,10 +141,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_many_kernel(const uint32_t
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < kB; ++j) {
-            const uint32_t w = word[j][t];
-            v4u sign;   // 2 is the code of 1, 10 that of -1
-#pragma unroll
-            for (int r = 0; r < 4; ++r) sign[r] = ((w << (3 - r)) & 0x88888888u) ^ 0xAAAAAAAAu;
+            const v4u sign = signs_of(word[j][t]);
 #pragma unroll
             for (int i = 0; i < kA; ++i) acc[i][j] = mfma<t>(x[t & 1][i], sign, acc[i][j], sx[i]);
         }
@@ -271,12 +252,6 @@ __global__ __launch_bounds__(kThreads, 2) void search_many_kernel(const uint32_t
             }
         }
     }
-}
-
-int range_of(int blocks) {
-    int r = 0;
-    while (((int64_t)blocks * 192 * 2 << (r + 1)) <= 1 << 24) ++r;
-    return r;
 }
 
 }  // namespace

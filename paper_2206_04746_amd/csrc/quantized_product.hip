@@ -14,17 +14,6 @@ namespace hdc {
 
 namespace {
 
-constexpr int kTile = 32;   // rows of either side to a matrix instruction
-
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef float v16f __attribute__((ext_vector_type(16)));
-
-template <int B>
-__device__ __forceinline__ v16f mfma(v4u a, v4u b, v16f c, uint32_t sa, uint32_t sb) {
-    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, B, (int)sa, B, (int)sb);
-}
-
 // Bytes [at, at + kBytes) of a row's scales as words; past the row's end those of 1.
 template <int kBytes>
 __device__ __forceinline__ void scale_bytes(const uint8_t *row, int at, int W, uint32_t (&out)[kBytes / 4]) {
@@ -47,23 +36,6 @@ __device__ __forceinline__ void scale_bytes(const uint8_t *row, int at, int W, u
 // ---- few rows: kSize of a by kSize of b a block, 32 or 16, a share of the dimensions to each of its waves
 constexpr int kFewWaves = 8;
 
-template <int kSize>
-struct FewSums;
-template <>
-struct FewSums<32> {
-    typedef v16f type;
-};
-template <>
-struct FewSums<16> {
-    typedef float type __attribute__((ext_vector_type(4)));
-};
-
-template <int B>
-__device__ __forceinline__ FewSums<16>::type mfma(v4u a, v4u b, FewSums<16>::type c, uint32_t sa, uint32_t sb) {
-    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, B, (int)sa, B, (int)sb);
-}
-
 // A wave takes the blocks of 32 dimensions of four matrix instructions at a time, four adjacent ones a lane, and then those that are as many
 // further on as the waves have.  Bound by the latency of its loads, 64 bytes of a row each.
 template <int kSize>
@@ -76,7 +48,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void product_few_kernel(const ui
     const int64_t m0 = (int64_t)blockIdx.y * kSize, n0 = (int64_t)blockIdx.x * kSize;
     const int64_t ra = min(m0 + col, M - 1) * W, rb = min(n0 + col, N - 1) * W;
     const v4u *const ca = reinterpret_cast<const v4u *>(a) + ra, *const cb = reinterpret_cast<const v4u *>(b) + rb;
-    typename FewSums<kSize>::type acc = {};
+    typename std::conditional<kSize == 32, v16f, v4f>::type acc = {};
     for (int u = wave * kPerUnit; u < W; u += waves * kPerUnit) {   // uniform
         const int first = u + 4 * group;
         v4u x[4], y[4];

@@ -21,43 +21,8 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = kWaves * kWave, kTile = 32;   // samples; most classes of a block
 constexpr int kMaxTiles = 32;                                      // of samples a block walks over once for every group of classes
-constexpr int kNoClass = 0x7FFFFFFF;
 
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef float v16f __attribute__((ext_vector_type(16)));
 
-// The largest difference of scales of so many blocks.
-constexpr int range_of(int blocks) {
-    int r = 0;
-    while ((int64_t)blocks * 192 * 2 << (r + 1) <= 1 << 24) ++r;
-    return r;
-}
-
-template <int B>
-__device__ __forceinline__ v16f mfma(v4u a, v4u b, v16f c, uint32_t scale) {
-    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, B, (int)scale, 0, 0x7F7F7F7F);
-}
-template <int B>
-__device__ __forceinline__ v4f mfma(v4u a, v4u b, v4f c, uint32_t scale) {
-    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, b8 = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, B, (int)scale, 0, 0x7F7F7F7F);
-}
-
-// +-1 of a word's 32 dimensions in the order of the codes: 2 is the code of 1, 10 that of -1.
-__device__ __forceinline__ v4u signs_of(uint32_t word) {
-    v4u out;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) out[r] = ((word << (3 - r)) & 0x88888888u) ^ 0xAAAAAAAAu;
-    return out;
-}
-
-struct Best {
-    double cos;
-    int c;
-};
-__device__ __forceinline__ Best better(Best a, Best b) { return b.cos > a.cos || (b.cos == a.cos && b.c < a.c) ? b : a; }
 
 // The best of a row of 16 lanes, in each of them: neighbours, their neighbours, halves of eight, halves of the row.
 template <int kSel>

@@ -292,6 +292,9 @@ int hdc_search_quantized(hdc_ctx *ctx, const uint32_t *hv_dev, int64_t N, const 
  * real-valued queries with class rows): out[m][n] = <a[m], b[n]>, fp32 sums.
  *   a_codes_dev [M][W][4], a_scales_dev [M][W], b_codes_dev [N][W][4], b_scales_dev [N][W],
  *   out_dev [M][N] fp32 out.  M == 0 or N == 0 is a successful no-op.  a and b may be the same rows.
+ * A sum is of eight or fewer fp32 sums where it is short of rows, of one otherwise: without rounding where
+ * it and what it adds fit 24 bits.  Products of two blocks below 2^-126 may count as 0, sums beyond fp32 are
+ * infinite, and what a block that is no number takes part in is no number.
  */
 int hdc_product_quantized(hdc_ctx *ctx, const uint32_t *a_codes_dev, const uint8_t *a_scales_dev, int64_t M,
                           const uint32_t *b_codes_dev, const uint8_t *b_scales_dev, int64_t N, float *out_dev,
@@ -333,7 +336,8 @@ int hdc_vsum(hdc_ctx *ctx, const uint32_t *hv_dev, int64_t N, int32_t *sum_dev, 
 /*
  * Labels outside [0, C) are a caller's mistake.  By default the training calls skip such samples
  * (defined behaviour, see hdc_train_classical).  With label checking on (a debugging aid, off by
- * default) hdc_train_classical, hdc_train_online and hdc_train_online_batched first count the
+ * default) hdc_train_classical, hdc_train_online, hdc_train_online_batched and
+ * hdc_train_online_quantized first count the
  * labels outside the range on `stream`, wait for the count (the call synchronises the stream)
  * and return HDC_ELABEL without training anything if there is one.
  */

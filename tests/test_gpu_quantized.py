@@ -220,7 +220,7 @@ def test_cosines_with_quantised_rows(N, C, D, kind):
 
 # many samples and classes: tiles of 128 classes and 256 samples, with some past their ends
 MANY = [(16500, 65, 500), (8200, 129, 300), (9000, 200, 1021), (3000, 1000, 257), (2049, 1024, 2081), (33000, 64, 225),
-        (25000, 65, 500), (12545, 129, 300), (13000, 200, 1021), (3100, 1024, 2081), (24577, 128, 4097), (33000, 1024, 290)]
+        (25000, 65, 500), (12545, 129, 300), (13000, 200, 1021), (3100, 1024, 2081), (24577, 128, 4097), (33000, 1024, 290), (26000, 100, 200)]
 
 
 @pytest.mark.parametrize("kind", ["normal", "zeros", "none", "orders"])
@@ -351,6 +351,16 @@ def run_training(hv, y, acc, batch, epochs, lr, reserve=True):
     return rows.cpu().numpy(), codes.cpu().numpy().view(np.uint32), scales.cpu().numpy(), norm.cpu().numpy()
 
 
+def check_batch(hv, y, acc, lr):
+    got, codes, scales, norm = run_training(hv, y, acc, len(y), 1, lr)
+    want, weights = oq.train_batch(hv, y, acc, lr)
+    assert np.all(np.abs(got.astype(np.float64) - want) <= 2.0 ** -24 * np.abs(want) * 2 + 2.0 ** -23 * weights[:, None])
+    # what is left is the quantisation of the rows that are left
+    want_codes, want_scales, _, want_norm = oq.quantize(got)
+    assert np.array_equal(codes, want_codes) and np.array_equal(scales, want_scales)
+    assert np.allclose(norm, want_norm, rtol=1e-12, atol=0)
+
+
 TRAIN = [(1, 1, 1), (3, 2, 31), (40, 5, 100), (64, 6, 1024), (100, 26, 500), (33, 40, 300), (1500, 20, 200), (2100, 6, 130), (500, 300, 96), (7, 3, 10000), (20000, 6, 130), (20000, 26, 97)]
 
 
@@ -363,13 +373,34 @@ def test_one_batch_of_training(N, C, D, start):
     acc = np.zeros((C, D), np.float32)
     if start == "sums":
         acc = np.rint(30 * rng.normal(size=(C, D))).astype(np.float32)
-    got, codes, scales, norm = run_training(hv, y, acc, N, 1, 0.7)
-    want, weights = oq.train_batch(hv, y, acc, 0.7)
-    assert np.all(np.abs(got.astype(np.float64) - want) <= 2.0 ** -24 * np.abs(want) * 2 + 2.0 ** -23 * weights[:, None])
-    # what is left is the quantisation of the rows that are left
-    want_codes, want_scales, _, want_norm = oq.quantize(got)
-    assert np.array_equal(codes, want_codes) and np.array_equal(scales, want_scales)
-    assert np.allclose(norm, want_norm, rtol=1e-12, atol=0)
+    check_batch(hv, y, acc, 0.7)
+
+
+@pytest.mark.parametrize("kind", ["normal", "orders"])
+@pytest.mark.parametrize("C", [7, 20, 40])
+@pytest.mark.parametrize("D", [2048, 2049, 4097, 6145, 8193, 10241, 12289, 14337, 16385, 20481])
+def test_every_length_of_rows(D, C, kind):
+    """Lengths around which more of a row is held at a time, and those that go in parts: searched and trained."""
+    rng = np.random.default_rng(D + C)
+    x = rows_of(kind, C, D, rng)
+    check_search(words(rng, 37, D), x)
+    check_batch(words(rng, 70, D), rng.integers(0, C, 70).astype(np.int32), x if kind == "normal" else np.clip(x, -1e6, 1e6), 0.5)
+
+
+def test_training_without_norms():
+    rng = np.random.default_rng(8)
+    N, C, D = 90, 6, 300
+    hv, y = words(rng, N, D), rng.integers(0, C, N).astype(np.int32)
+    acc = np.rint(10 * rng.normal(size=(C, D))).astype(np.float32)
+    want = run_training(hv, y, acc, 32, 2, 1.0)
+    ctx = context(D, C)
+    rows = torch.from_numpy(acc.copy()).cuda()
+    codes, scales = torch.zeros((C, 40), dtype=torch.int32, device="cuda"), torch.zeros((C, 10), dtype=torch.uint8, device="cuda")
+    ctx.hdc_train_online_quantized(dev_u32(hv), torch.from_numpy(y).cuda(), rows, codes, scales, None, 32, 2, 1.0)
+    torch.cuda.synchronize()
+    ctx.close()
+    assert np.array_equal(rows.cpu().numpy(), want[0]) and np.array_equal(codes.cpu().numpy().view(np.uint32), want[1])
+    assert np.array_equal(scales.cpu().numpy(), want[2])
 
 
 @pytest.mark.parametrize("N,C,D,batch,epochs", [(50, 3, 200, 16, 2), (300, 26, 333, 64, 1), (70, 2, 64, 1, 1)])

@@ -303,8 +303,8 @@ int hdc_product_quantized(hdc_ctx *ctx, const uint32_t *a_codes_dev, const uint8
 /*
  * hdc_train_online_batched for a model that will answer with quantised rows: before every batch the
  * rows are quantised as by hdc_quantize, the samples of the batch are scored against the quantised rows
- * (cos_c of hdc_search_quantized, pred and the two fp32 weights as there), and the update goes to
- * the fp32 rows unchanged: acc[c] = float(double(acc[c]) + delta[c]).  After the last batch codes_dev,
+ * (cos_c of hdc_search_quantized, pred and the two fp32 weights as there; no pred where all cosines are
+ * no numbers), and the update goes to the fp32 rows unchanged: acc[c] = float(double(acc[c]) + delta[c]).  After the last batch codes_dev,
  * scales_dev and norm_dev (NULL if not wanted) hold the rows as they are then, quantised.
  *   acc_dev [C][D] fp32 in/out, codes_dev [C][W][4], scales_dev [C][W], norm_dev [C] out (and used
  *   in between).  N == 0 or epochs == 0 leaves all four as they are.

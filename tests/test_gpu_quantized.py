@@ -387,6 +387,29 @@ def test_every_length_of_rows(D, C, kind):
     check_batch(words(rng, 70, D), rng.integers(0, C, 70).astype(np.int32), x if kind == "normal" else np.clip(x, -1e6, 1e6), 0.5)
 
 
+@pytest.mark.parametrize("N,C,D", [(60, 6, 300), (60, 20, 300), (1200, 20, 300), (60, 40, 300)])
+def test_training_with_rows_that_are_no_numbers(N, C, D):
+    """Such a row is never predicted, its own samples make all of it no numbers, the others are trained as ever; of all such rows none is predicted."""
+    rng = np.random.default_rng(N + C)
+    hv, y = words(rng, N, D), rng.integers(0, C, N).astype(np.int32)
+    acc = np.rint(10 * rng.normal(size=(C, D))).astype(np.float32)
+    acc[1, 40], acc[2, 299] = np.inf, np.nan
+    got, codes, scales, norm = run_training(hv, y, acc, N, 1, 0.7)
+    want, weights = oq.train_batch(hv, y, acc, 0.7)
+    # (a class without samples keeps its row)
+    assert all(np.isnan(got[c]).all() if np.any(y == c) else np.array_equal(got[c], acc[c], equal_nan=True) for c in (1, 2))
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    fine = np.arange(C) != 1
+    fine[2] = False
+    assert np.all(np.abs(got.astype(np.float64) - want)[fine] <= (2.0 ** -24 * np.abs(want) * 2 + 2.0 ** -23 * weights[:, None])[fine])
+    want_codes, want_scales, _, _ = oq.quantize(got)
+    assert np.array_equal(codes, want_codes) and np.array_equal(scales, want_scales) and np.isnan(norm[1:3]).all() and np.isfinite(norm[fine]).all()
+    acc[:, 7] = np.inf
+    got = run_training(hv, np.where(y == 3, 4, y).astype(np.int32), acc, N, 1, 0.7)[0]
+    with np.errstate(invalid="ignore"):
+        assert np.array_equal(got[3], acc[3])       # nothing was added, nothing taken away
+
+
 def test_training_without_norms():
     rng = np.random.default_rng(8)
     N, C, D = 90, 6, 300

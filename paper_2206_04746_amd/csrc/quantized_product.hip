@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void product_few_kernel(const ui
     }
 }
 
-// ---- many rows: a tile of 64 kA rows of a by 64 kB of b a block of two by two waves
+// ---- many rows: a tile of 64 kA rows of a by 64 kB of b a block, or each of its groups, of two by two waves
 constexpr int kThreads = 256, kStep = 8, kUnit = 16;   // blocks of 32 dimensions a step, bytes of one
 
 // The sums of a tile are computed here, and not past the next barrier: operands take the registers of those that have been multiplied.
@@ -94,18 +94,23 @@ __device__ __forceinline__ v16f settled(v16f v) {
 // Steps of 256 dimensions.  While a step's matrix instructions are issued, four groups of kA kB, the operands of each next group are read
 // from LDS and, once all of the step's are in registers, the step after next is asked for in its place: all of it a piece to a
 // matrix instruction, so that these follow one another without a pause.  W >= 2 kStep.
-template <int kA, int kB>
-__global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
+//
+// kSplit > 1: the dimensions are shared out to as many groups of four waves, whose sums meet in LDS.
+template <int kA, int kB, int kSplit>
+__global__ __launch_bounds__(kThreads *kSplit, kA * kB > 4 ? 1 : 2) void product_tiles_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
                                                                                       const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb,
                                                                                       int64_t N, int W, int tiles_m, int tiles_n, float *__restrict__ out) {
     constexpr int kRowsA = 64 * kA, kRowsB = 64 * kB, kRows = kRowsA + kRowsB;
-    constexpr int kOwn = kRows / kThreads, kLoads = kRows / 32, kPer = kLoads / (kA * kB);   // rows whose scales a thread brings; loads of a step, and to a matrix instruction
+    constexpr int kOwn = (kRows + kThreads - 1) / kThreads, kLoads = kRows / 32, kPer = kLoads / (kA * kB);   // rows whose scales a thread brings; loads of a step, and to a matrix instruction
     static_assert(kLoads % (kA * kB) == 0 && kA + kB <= 2 * kA * kB, "pieces to a matrix instruction");
     // Codes of a step and of the next: block k of a row's eight is at place k ^ (row / 2 % 8) of the row, so that sixteen rows' blocks lie in
     // different banks.  Scales of two steps and of the next two.
-    __shared__ __align__(16) uint32_t unit[2][kRows * kStep * 4];
-    __shared__ uint32_t scale[2][4][kRows];
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+    __shared__ __align__(16) uint32_t units[kSplit][2][kRows * kStep * 4];
+    __shared__ uint32_t scales[kSplit][2][4][kRows];
+    const int part = kSplit > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads) : 0;
+    uint32_t(*const unit)[kRows * kStep * 4] = units[part];
+    uint32_t(*const scale)[4][kRows] = scales[part];
+    const int tid = kSplit > 1 ? threadIdx.x % kThreads : threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
 
     // Blocks of consecutive numbers go to the eight dies in turn: a die takes tiles that lie together, eight rows of tiles wide.
     int tm, tn;
@@ -118,7 +123,8 @@ __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_k
     const int64_t m0 = (int64_t)tm * kRowsA, n0 = (int64_t)tn * kRowsB;
     const int rows_a = (int)min((int64_t)kRowsA, M - m0), rows_b = (int)min((int64_t)kRowsB, N - n0);
     const uint32_t pitch = (uint32_t)W * kUnit;
-    const int steps = (W + kStep - 1) / kStep;
+    // A group's steps: an even number if there are several groups, so that none begins between two steps whose scales come together.
+    const int all = (W + kStep - 1) / kStep, steps = kSplit > 1 ? (all + 2 * kSplit - 1) / (2 * kSplit) * 2 : all, first = part * steps;
     const LdsSource from_a = lds_source(a + m0 * W * 4, (uint32_t)rows_a * pitch), from_b = lds_source(b + n0 * W * 4, (uint32_t)rows_b * pitch);
 
     // A step's blocks, or the row's last eight: those that the step before has had are zeros then.
@@ -150,7 +156,8 @@ __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_k
 #pragma unroll
         for (int i = 0; i < kOwn; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) scale[to][j][tid + i * kThreads] = piece[i][j];
+            for (int j = 0; j < 4; ++j)
+                if (kRows % kThreads == 0 || tid + i * kThreads < kRows) scale[to][j][tid + i * kThreads] = piece[i][j];
     };
 
     const int wm = (wave >> 1) * 32 * kA, wn = kRowsA + (wave & 1) * 32 * kB;   // this wave's rows
@@ -200,7 +207,8 @@ __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_k
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         const int again = step * kStep - begin_of(step);   // blocks that the step before has had: of the last step, and past it
-        if (again > 0) {
+        const int latest = step + (kSplit - 1 - part) * steps;
+        if (latest * kStep > begin_of(latest)) {           // for all of the block's threads or none, the last group's
             for (int u = tid; u < kRows * kStep; u += kThreads)
                 if (((u & 7) ^ (u >> 4 & 7)) < again) *reinterpret_cast<v4u *>(unit[step & 1] + u * 4) = v4u{0, 0, 0, 0};
             __syncthreads();
@@ -225,21 +233,42 @@ __global__ __launch_bounds__(kThreads, kA * kB > 4 ? 1 : 2) void product_tiles_k
         });
     };
 
-    ask_scales(0);
+    ask_scales(first);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(i, unit[0], (uint32_t)begin_of(0));
-    put_scales(0);
-    meet(0);
+    for (int i = 0; i < kLoads; ++i) load(i, unit[0], (uint32_t)begin_of(first));
+    put_scales(first / 2 & 1);
+    meet(first);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(i, unit[1], (uint32_t)begin_of(1));
-    take_scales(0, 0);
+    for (int i = 0; i < kLoads; ++i) load(i, unit[1], (uint32_t)begin_of(first + 1));
+    take_scales(first, 0);
 #pragma unroll
     for (int i = 0; i < kA + kB; ++i) take(0, 0, i);
-    for (int k = 0; k < steps; k += 2) {   // (a step past the last is one of zeros)
+    for (int k = first; k < first + steps; k += 2) {   // (a step past the last is one of zeros)
         go(k, std::integral_constant<int, 0>{});
         go(k + 1, std::integral_constant<int, 1>{});
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing may be on its way into LDS when the block's is given to another)
+    if constexpr (kSplit > 1) {
+        constexpr int kRow = 64 * kB;
+        static_assert(kRowsA * kRow <= 2 * kRows * kStep * 4, "a group's sums take its codes' place");
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kA; ++i)
+#pragma unroll
+            for (int j = 0; j < kB; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    reinterpret_cast<float *>(unit[0])[(wm + i * 32 + 8 * (r / 4) + 4 * half + r % 4) * kRow + wn - kRowsA + j * 32 + col] = acc[i][j][r];
+        __syncthreads();
+        for (int at = threadIdx.x; at < kRowsA * kRow; at += kThreads * kSplit) {
+            const int row = at / kRow, n = at % kRow;
+            double sum = 0.0;   // of the groups' fp32 sums, rounded once
+#pragma unroll
+            for (int q = 0; q < kSplit; ++q) sum += (double)reinterpret_cast<const float *>(units[q])[at];
+            if (row < rows_a && n < rows_b) out[(m0 + row) * N + n0 + n] = (float)sum;
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < kA; ++i)
 #pragma unroll
@@ -261,13 +290,17 @@ int launch_product_quantized(hdc_ctx_impl *c, const uint32_t *a, const uint8_t *
                              hipStream_t s) {
     ProfScope prof(c, HDC_K_PRODUCT_QUANTIZED, s);
     const int W = c->W;
-    const int64_t fewest = ((M + 15) / 16) * ((N + 15) / 16), few = ((M + 31) / 32) * ((N + 31) / 32), large = ((M + 255) / 256) * ((N + 255) / 256), small = ((M + 127) / 128) * ((N + 127) / 128);
-    // Few rows up to as many blocks as compute units, in 16 by 16 up to as many blocks of these; tiles of 128 rows up to two a unit, tiles of
-    // 256 beyond.  us a call, 16 by 16 / 32 by 32: 64 by 64 rows of 9999 6.6 9.9, 1559 by 26 6.8 9.8 (196 blocks of 16 by 16); 96 by 1000 14.2
-    // 10.5 (378), 512 by 512 21 13.5, of 16384 40 23.  us, few / 128 / 256: 512 by 512 rows of 9999 13.5 26.8 64; 1000 by 1000 of 9999 88 44 83,
-    // of 1000 14.2 8.7 20.7; 8192 by 1024 of 9999 685 73 89; 3000 by 3000 of 9999 885 109 91; 4096 by 4096 of 9999 1358 146 115, of 1000
-    // 174 25.1 24.9.
-    if (few <= c->num_cus || W < 2 * kStep) {
+    auto blocks = [&](int64_t size) { return ((M + size - 1) / size) * ((N + size - 1) / size); };
+    // Few rows up to as many blocks as compute units, in 16 by 16 up to as many blocks of these; then tiles of 64 rows, two shares of the
+    // dimensions a block, up to two blocks a unit (its LDS), tiles of 128 up to two, tiles of 256 beyond.  us a call:
+    //   16 by 16 / 32 by 32: 64 by 64 rows of 9999 6.6 9.9, 1559 by 26 6.8 9.8 (196 blocks of 16 by 16), 96 by 1000 14.2 10.5 (378), 512 by 512
+    //   21 13.5 (1024), of 16384 40 23
+    //   32 by 32 / 64: 512 by 512 rows of 9999 13.7 17.7 (256 blocks of 32 by 32), 600 by 600 30 19 (361), 1000 by 1000 54 25, of 4096 22 10.4, of 1000
+    //   9.1 7.1
+    //   64 / 128: 1000 by 1000 rows of 9999 25 45 (256 blocks of 64), 1300 by 1300 35 45 (441), 1500 by 1500 58 46 (576), of 4096 22 17.6, of 1000
+    //   11.9 9.8; in four shares 1000 by 1000 of 9999 24, 1300 by 1300 45
+    //   128 / 256: 2000 by 2000 rows of 9999 50 86 (256 blocks of 128), 3000 by 3000 109 90 (576), of 1000 19.8 23.2, 4096 by 4096 of 9999 135 104
+    if (blocks(32) <= c->num_cus || W < 2 * kStep) {
         auto launch = [&](auto kernel, int size) {
             const int per = 4 * kWave / size, waves = std::min((W + per - 1) / per, kFewWaves);
             for (int64_t m = 0; m < M; m += (int64_t)size * 65535) {
@@ -276,16 +309,21 @@ int launch_product_quantized(hdc_ctx_impl *c, const uint32_t *a, const uint8_t *
                                    a + m * W * 4, sa + m * W, rows, b, sb, N, W, out + m * N);
             }
         };
-        if (fewest <= c->num_cus)
+        if (blocks(16) <= c->num_cus)
             launch(product_few_kernel<16>, 16);
         else
             launch(product_few_kernel<32>, 32);
-    } else if (small > 2 * (int64_t)c->num_cus) {
-        hipLaunchKernelGGL((product_tiles_kernel<4, 4>), dim3((unsigned)large), dim3(kThreads), 0, s, a, sa, M, b, sb, N, W, (int)((M + 255) / 256),
-                           (int)((N + 255) / 256), out);
     } else {
-        hipLaunchKernelGGL((product_tiles_kernel<2, 2>), dim3((unsigned)small), dim3(kThreads), 0, s, a, sa, M, b, sb, N, W, (int)((M + 127) / 128),
-                           (int)((N + 127) / 128), out);
+        auto launch = [&](auto kernel, int size, int split) {
+            const int64_t tiles_m = (M + size - 1) / size, tiles_n = (N + size - 1) / size;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(kThreads * split), 0, s, a, sa, M, b, sb, N, W, (int)tiles_m, (int)tiles_n, out);
+        };
+        if (blocks(64) <= 2 * (int64_t)c->num_cus)
+            launch(product_tiles_kernel<1, 1, 2>, 64, 2);
+        else if (blocks(128) <= 2 * (int64_t)c->num_cus)
+            launch(product_tiles_kernel<2, 2, 1>, 128, 1);
+        else
+            launch(product_tiles_kernel<4, 4, 1>, 256, 1);
     }
     HDC_HIP(hipGetLastError());
     return HDC_OK;

@@ -1,9 +1,11 @@
 // Cosine inference with class rows of 4-bit floats (arXiv 2206.04746, Sec. III), and the dot products of online training with them.
 //
 // The matrix cores take such rows as they are, with their scales (v_mfma_scale_f32_32x32x64_f8f6f4), and a sample's bits as +-1 in the
-// same format.  A block of eight waves takes 32 classes, or the model's up to 16, and walks over the samples, 32 at a time; each wave has an eighth of the
-// dimensions and holds the codes of its classes there in registers, so that all there is to read on the way is the samples, once.
-// The waves' parts of the dot products meet in LDS.
+// same format.  A block of eight waves takes 32 classes, or the model's up to 16, and walks over the samples, 32 at a time; each wave has
+// an eighth of the dimensions and holds the codes of its classes there in registers, so that all there is to read on the way is the
+// samples, once.  The waves' parts of the dot products meet in LDS.  Where a row is short and samples are many, four, two or one of
+// the waves hold it, and the block takes two, four or eight times 32 samples at once, for one barrier and with fewer lanes a sample at the end.
+// 200000 samples of 10000 dimensions, 26 classes: 65 us (3.9 TB/s of words), 1000000 of 1000: 54.
 //
 // Sums without rounding: the products of a row are whole multiples of half its smallest scale, and a block of 32 dimensions gives at
 // most 192 (32 times 6) of the largest.  Where a row's scales lie no further apart than 2^kRange, sums over it fit the 24 bits of
@@ -48,13 +50,13 @@ __device__ __forceinline__ double sum_of_16(double v) {
     return v + from(v, std::integral_constant<int, kMirrorRow>{});
 }
 
-// grid (runs of `tiles` tiles of samples, splits of the groups of 32 classes).
+// kShare waves hold a row.  grid (runs of `tiles` tiles of samples, a multiple of kWaves / kShare; splits of the groups of classes).
 //   kNearest  cos_out (or null) takes the cosines, and the nearest class of a block's own goes to pred_out or, if that is null, to best_cos and
 //             best_c [split][N]
 //   kDots     part[n][C] takes the dot products
 //   kWeights  up to 32 classes: the weights of online training (`weigh`); the last weigh.tblocks blocks transpose the samples' bits
 enum Mode { kNearest, kDots, kWeights };
-template <int kClasses, int kSteps, bool kParts, int kMode>
+template <int kClasses, int kSteps, int kShare, bool kParts, int kMode>
 __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uint32_t *__restrict__ hv, int64_t N, int W, int C,
                                                                        const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                                        const double *__restrict__ norm, double root_d, int tiles, int groups,
@@ -62,13 +64,16 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
                                                                        int32_t *__restrict__ pred_out, double *__restrict__ best_cos, int *__restrict__ best_c,
                                                                        QuantWeights weigh, const int *__restrict__ wide) {
     constexpr int kPieces = kWave / kClasses, kCols = kTile / kClasses, kOwn = kClasses / 16;   // lanes to a row; rows of samples to a lane; classes of a thread
-    constexpr int kBlocks = kWaves * kPieces * kSteps, kRange = range_of(kBlocks);              // of a row at a time
+    constexpr int kBlocks = kShare * kPieces * kSteps, kRange = range_of(kBlocks);              // of a row at a time
+    constexpr int kAtOnce = kWaves / kShare;                                                    // tiles of samples
+    static_assert(kShare == kWaves || (!kParts && kMode == kNearest), "shares of short rows");
     typedef typename std::conditional<kClasses == 32, v16f, v4f>::type Sums;
     constexpr int kPitch = kTile + 4;                                          // (sixteen classes by four samples lie in different banks)
     __shared__ float sums[2][kWaves][kTile][kPitch];
     __shared__ int limits[2][kWaves][kTile];                    // largest and smallest scale of a class in a wave's dimensions
     __shared__ double run_cos[kMode == kNearest ? kMaxTiles * kTile : kTile];   // the nearest of the groups before; kWeights: norms of the classes
     __shared__ int run_c[kMode == kNearest ? kMaxTiles * kTile : 1];
+    __shared__ double ratio[kShare < kWaves ? kClasses : 1];    // unit by size
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, col = lane % kClasses, piece = lane / kClasses;
     if constexpr (kMode == kWeights) {
         const int idx = (int)blockIdx.x - ((int)gridDim.x - weigh.tblocks);
@@ -87,34 +92,35 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         }
     }
     const int64_t all = kMode == kWeights ? weigh.ld / kTile : (N + kTile - 1) / kTile, tile0 = (int64_t)blockIdx.x * tiles;
-    const int count = (int)min((int64_t)tiles, all - tile0), parts = kParts ? (W + kBlocks - 1) / kBlocks : 1;
+    const int count = (int)((min((int64_t)tiles, all - tile0) + kAtOnce - 1) / kAtOnce), parts = kParts ? (W + kBlocks - 1) / kBlocks : 1;
     const int g0 = blockIdx.y * groups, g1 = min(g0 + groups, (C + kClasses - 1) / kClasses);
 
     v4u code[kSteps];
     uint32_t scale[kSteps / 4];   // a byte a step, less `top` (modulo 2^32, all four together): 127 for the row's largest
     int top = 0, passes = 1;      // the row's largest scale less 127; passes that the block needs
-    double unit[kOwn], size[kOwn];   // of this thread's classes: the largest scale, the row's norm times that of a sample
+    double unit[kOwn], size[kOwn];   // of this thread's classes: the largest scale; the row's norm times that of a sample (kNearest: 1 by it, or 0)
     const int n_of = tid >> 4, c_of = tid & 15;   // this thread's sample of a tile, and the first of its classes, which are 16 apart
     constexpr int kAhead = !kParts && kSteps <= 20 ? 1 : 0;   // words of the next sample asked for before this one's products, or after them
     uint32_t word[1 + kAhead][kCols][kSteps];
 
-    // A wave's blocks of part z are [w0, w0 + kPieces kSteps), those before the row's end; it takes the row's last ones where that is nearer, so
-    // that its loads need no limits, with codes of zero for the others'.  (Rows shorter than that: one by one, the last again.)
-    // Step t has block kPieces (t & ~3) + 4 piece + t % 4 from there: a load of four words is 16 kPieces bytes of kClasses rows.
-    const bool whole = W >= kPieces * kSteps;
-    auto begin_of = [&](int z) { return min(z * kBlocks + wave * kPieces * kSteps, W - kPieces * kSteps); };
+    // This wave's tile of those at once, and its share of the row: of part z its blocks are those from share_of(z) on.  Step t has block kPieces
+    // (t & ~3) + 4 piece + t % 4 from there, a load of four words is 16 kPieces bytes of kClasses rows; where the row ends before, the
+    // row's last four, so that loads need no limits, with codes of zero for those that are not theirs.  (Rows shorter than that: one by one.)
+    const int tile = wave / kShare, share = wave % kShare;
+    const bool whole = W >= 4;
+    auto share_of = [&](int z) { return z * kBlocks + share * kPieces * kSteps; };
     // Words of sample tile i in part z of the row.
     auto ask = [&](int i, int z, uint32_t(&to)[kCols][kSteps]) {
 #pragma unroll
         for (int k = 0; k < kCols; ++k) {
-            const int64_t n = min((tile0 + i) * kTile + kClasses * k + col, N - 1);
+            const int64_t n = min((tile0 + i * kAtOnce + tile) * kTile + kClasses * k + col, N - 1);
             const uint32_t *const from = hv + n * W;
             if (whole) {
-                const int w0 = begin_of(z) + 4 * piece;
+                const int w0 = share_of(z) + 4 * piece;
 #pragma unroll
-                for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&to[k][t], from + w0 + kPieces * t, 16);
+                for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&to[k][t], from + min(w0 + kPieces * t, W - 4), 16);
             } else {
-                const int here = anew(wave * kPieces * kSteps + 4 * piece);   // (no places in the row are kept)
+                const int here = anew(share * kPieces * kSteps + 4 * piece);   // (no places in the row are kept)
 #pragma unroll
                 for (int t = 0; t < kSteps; ++t) {
                     to[k][t] = from[min(here + kPieces * (t & ~3) + t % 4, W - 1)];
@@ -126,20 +132,21 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     // This wave's codes of a group of classes in part z; meanwhile() is done while they are on their way.  (Classes past the last are that one
     // again.)
     auto hold = [&](int group, int z, auto meanwhile) {
-        const int w0 = z * kBlocks + wave * kPieces * kSteps;
+        const int w0 = share_of(z);
         const int64_t from = anew((int64_t)min(group * kClasses + col, C - 1) * W);
         const v4u *const here = reinterpret_cast<const v4u *>(codes) + from;
         if (whole) {
-            const int begin = begin_of(z), first = begin + 4 * piece;
+            const int first = w0 + 4 * piece;
 #pragma unroll
-            for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&scale[t / 4], scales + from + first + kPieces * t, 4);
+            for (int t = 0; t < kSteps; t += 4) __builtin_memcpy(&scale[t / 4], scales + from + min(first + kPieces * t, W - 4), 4);
 #pragma unroll
-            for (int t = 0; t < kSteps; ++t) code[t] = here[first + kPieces * (t & ~3) + t % 4];
-            if (begin < w0) {   // blocks before w0 are another wave's
+            for (int t = 0; t < kSteps; ++t) code[t] = here[min(first + kPieces * (t & ~3), W - 4) + t % 4];
+            if (w0 + kPieces * kSteps > W) {   // blocks before a step's own are another's
                 const int place = anew(first);
 #pragma unroll
                 for (int t = 0; t < kSteps; ++t) {
-                    const bool mine = place + kPieces * (t & ~3) + t % 4 >= w0;
+                    const int own = place + kPieces * (t & ~3);
+                    const bool mine = min(own, W - 4) + t % 4 >= own;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) code[t][r] = mine ? code[t][r] : 0u;
                     scale[t / 4] &= mine ? ~0u : ~(255u << 8 * (t & 3));
@@ -190,7 +197,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         if (piece == 0) limits[0][wave][col] = most, limits[1][wave][col] = least;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) most = max(most, limits[0][w][col]), least = min(least, limits[1][w][col]);
+        for (int w = 0; w < kShare; ++w) most = max(most, limits[0][w][col]), least = min(least, limits[1][w][col]);
         passes = most < 0 || most == kQuantNone ? 1 : (most - least) / (kRange + 1) + 1;   // (of a row that is no number, any)
         for (int off = 1; off < kClasses; off <<= 1) passes = max(passes, __shfl_xor(passes, off, kWave));
         passes = __builtin_amdgcn_readfirstlane(passes);
@@ -205,7 +212,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         for (int j = 0; j < kOwn; ++j) {
             int largest = -1;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) largest = max(largest, limits[0][w][c_of + 16 * j]);
+            for (int w = 0; w < kShare; ++w) largest = max(largest, limits[0][w][c_of + 16 * j]);
             unit[j] = largest < 0 ? 1.0 : scale_value(largest);
         }
     };
@@ -234,15 +241,29 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
             for (int j = 0; j < kClasses * kClasses / kWave; ++j) to[4 * kPieces * (j / 4) + 4 * piece + j % 4][kClasses * k + col] = acc[k][j];
         }
     };
-    auto sum_of = [&](int turn, int j) {
+    auto sum_of = [&](int turn, int q, int j) {   // of tile q
         float sum = 0.0f;   // without rounding
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) sum += sums[turn][w][c_of + 16 * j][n_of];
+        for (int w = 0; w < kShare; ++w) sum += sums[turn][q * kShare + w][c_of + 16 * j][n_of];
         return sum;
+    };
+    // The nearest of a group of classes for the block's sample `at`, which is n.
+    auto keep = [&](int g, int at, int64_t n, Best best) {
+        if (g > g0) best = better(Best{run_cos[at], run_c[at]}, best);
+        if (g + 1 < g1) {
+            run_cos[at] = best.cos, run_c[at] = best.c;
+        } else if (n < N) {
+            if (pred_out) {
+                pred_out[n] = best.c == kNoClass ? 0 : best.c;
+            } else {
+                best_cos[(int64_t)blockIdx.y * N + n] = best.cos;
+                best_c[(int64_t)blockIdx.y * N + n] = best.c;
+            }
+        }
     };
     auto finish = [&](int g, int i, const double(&total)[kOwn]) {
         const int c = g * kClasses + c_of;
-        const int64_t n = (tile0 + i) * kTile + n_of;
+        const int64_t n = (tile0 + i) * kTile + n_of;   // tile i of the block
         if constexpr (kMode == kDots) {
 #pragma unroll
             for (int j = 0; j < kOwn; ++j)
@@ -275,26 +296,31 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
 #pragma unroll
             for (int j = 0; j < kOwn; ++j)
                 if (c + 16 * j < C) {
-                    const double cs = size[j] == 0.0 ? 0.0 : total[j] / size[j];
+                    const double cs = total[j] * size[j];
                     if (cos_out && n < N) cos_out[n * C + c + 16 * j] = (float)cs;
                     best = better(best, Best{cs, c + 16 * j});
                 }
             best = best_of_16(best);
-            if (c_of == 0) {
-                const int at = i * kTile + n_of;
-                if (g > g0) best = better(Best{run_cos[at], run_c[at]}, best);
-                if (g + 1 < g1) {
-                    run_cos[at] = best.cos, run_c[at] = best.c;
-                } else if (n < N) {
-                    if (pred_out) {
-                        pred_out[n] = best.c == kNoClass ? 0 : best.c;
-                    } else {
-                        best_cos[(int64_t)blockIdx.y * N + n] = best.cos;
-                        best_c[(int64_t)blockIdx.y * N + n] = best.c;
-                    }
-                }
-            }
+            if (c_of == 0) keep(g, i * kTile + n_of, n, best);
         }
+    };
+    // All of the tiles at once without their cosines: kLanes lanes a sample.
+    constexpr int kLanes = 16 / kAtOnce;
+    auto finish_all = [&](int g, int i) {
+        const int at = tid / kLanes, lane_of = tid % kLanes;
+        Best best = {-__builtin_inf(), kNoClass};
+#pragma unroll 4
+        for (int c = lane_of; c < kClasses; c += kLanes) {
+            float sum = 0.0f;   // without rounding
+#pragma unroll
+            for (int w = 0; w < kShare; ++w) sum += sums[i & 1][at / kTile * kShare + w][c][at % kTile];
+            const double cs = (double)sum * ratio[c];
+            if (cs > best.cos && g * kClasses + c < C) best = {cs, g * kClasses + c};
+        }
+        if constexpr (kLanes > 1) best = better(best, of_lane<0xB1>(best));
+        if constexpr (kLanes > 2) best = better(best, of_lane<0x4E>(best));
+        if constexpr (kLanes > 4) best = better(best, of_lane<0x141>(best));
+        if (lane_of == 0) keep(g, i * kAtOnce * kTile + at, (tile0 + i * kAtOnce) * kTile + at, best);
     };
 
     constexpr int kEarly = kMode == kWeights ? 16 : 1;   // partial norms asked for first
@@ -327,7 +353,11 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
             for (int j = 0; j < kOwn; ++j) size[j] = run_cos[c_of + 16 * j];
         }
 #pragma unroll
-        for (int j = 0; j < kOwn; ++j) size[j] = sqrt(size[j]) * root_d;
+        for (int j = 0; j < kOwn; ++j) {
+            size[j] = sqrt(size[j]) * root_d;
+            if constexpr (kMode == kNearest) size[j] = size[j] == 0.0 ? 0.0 : 1.0 / size[j];
+            if (kAtOnce > 1 && n_of == 0) ratio[c_of + 16 * j] = unit[j] * size[j];
+        }
         if constexpr (!kParts) {
             if (__builtin_expect(passes == 1, 1)) {
                 // A tile is finished while the next one's products are formed, by half of the waves before and by the other half after their own:
@@ -335,10 +365,17 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
                 const int one = anew(1);   // (no loop of its own for the first tile)
                 for (int i = 0; i <= count; ++i) {
                     auto before = [&]() {
-                        double total[kOwn];
+                        if (kAtOnce > 1 && !cos_out) {
+                            finish_all(g, i - 1);
+                            return;
+                        }
+#pragma unroll 1
+                        for (int q = 0; q < kAtOnce; ++q) {
+                            double total[kOwn];
 #pragma unroll
-                        for (int j = 0; j < kOwn; ++j) total[j] = (double)sum_of((i - 1) & 1, j) * unit[j];
-                        finish(g, i - 1, total);
+                            for (int j = 0; j < kOwn; ++j) total[j] = (double)sum_of((i - 1) & 1, q, j) * unit[j];
+                            finish(g, (i - 1) * kAtOnce + q, total);
+                        }
                     };
                     if (i >= one && wave < kWaves / 2) before();
                     if (i < count) {
@@ -364,7 +401,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
         }
         int turn = 0;
         for (int i = 0; i < count; ++i) {
-            double total[kOwn] = {};
+            double total[kAtOnce][kOwn] = {};
             for (int z = 0; z < parts; ++z) {
                 if constexpr (kParts) hold(g, z, []() {});
                 double down = 1.0;
@@ -387,14 +424,17 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
                     put(turn, acc);
                     __syncthreads();
 #pragma unroll
-                    for (int j = 0; j < kOwn; ++j) total[j] = fma((double)sum_of(turn, j), unit[j] * down, total[j]);
+                    for (int q = 0; q < kAtOnce; ++q)
+#pragma unroll
+                        for (int j = 0; j < kOwn; ++j) total[q][j] = fma((double)sum_of(turn, q, j), unit[j] * down, total[q][j]);
                     turn ^= 1;
                     down *= 1.0 / (2 << kRange);
                 }
                 const bool last = z + 1 == parts;
                 ask(last ? (i + 1 < count ? i + 1 : 0) : i, last ? 0 : z + 1, word[0]);
             }
-            finish(g, i, total);
+#pragma unroll
+            for (int q = 0; q < kAtOnce; ++q) finish(g, i * kAtOnce + q, total[q]);
         }
     }
 }
@@ -408,40 +448,76 @@ __global__ __launch_bounds__(256) void nearest_kernel(const double *__restrict__
     pred[n] = best.c == kNoClass ? 0 : best.c;
 }
 
-// Classes of a block: for no more than 16 (v_mfma_scale_f32_16x16x128_f8f6f4) half of the loads and registers (2947 samples of 10000 with 6
-// classes 6.9 us a call, in a block for 32 7.7; a batch of 64 in training 8.5 us, 8.9).
-int quantized_classes(const hdc_ctx_impl *c) { return c->p.C > 16 ? 32 : 16; }
+// Classes of a block and the waves that share a row: for no more than 16 classes (v_mfma_scale_f32_16x16x128_f8f6f4) half of the loads and
+// registers (2947 samples of 10000 with 6 classes 6.9 us a call, in a block for 32 7.7; a batch of 64 in training 8.5 us, 8.9).
+struct Form {
+    int classes, share;
+};
 
 template <int kMode>
-void launch(hdc_ctx_impl *c, dim3 grid, hipStream_t s, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
+void launch(hdc_ctx_impl *c, Form form, dim3 grid, hipStream_t s, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
             int tiles, int groups, double *part, float *cos_out, int32_t *pred, double *best_cos, int *best_c, const QuantWeights &weigh = {}, const int *wide = nullptr) {
-#define HDC_SEARCH(CLASSES, STEPS, PARTS)                                                                                                             \
-    hipLaunchKernelGGL((search_quantized_kernel<CLASSES, STEPS, PARTS, kMode>), grid, dim3(kThreads), 0, s, hv, N, c->W, c->p.C, codes, scales, norm, \
+#define HDC_SEARCH(CLASSES, STEPS, SHARE, PARTS)                                                                                                             \
+    hipLaunchKernelGGL((search_quantized_kernel<CLASSES, STEPS, SHARE, PARTS, kMode>), grid, dim3(kThreads), 0, s, hv, N, c->W, c->p.C, codes, scales, norm, \
                        sqrt((double)c->p.D), tiles, groups, part, cos_out, pred, best_cos, best_c, weigh, wide)
     // Steps of a wave: as many as a row needs, up to 20 or 28 (the registers); rows of more than that go in parts of 16.
-    const int classes = quantized_classes(c), blocks = kWaves * (kWave / classes), steps = ((c->W + blocks - 1) / blocks + 3) / 4 * 4;
-    if (classes == 16) {
+    const int blocks = form.share * (kWave / form.classes), steps = ((c->W + blocks - 1) / blocks + 3) / 4 * 4;
+    if constexpr (kMode == kNearest) {
+#define HDC_SEARCH_SHORT(CLASSES)                                                                              \
+    switch (form.share * 100 + std::max(steps, form.share == 1 ? 8 : 12)) {                                    \
+        case 108: HDC_SEARCH(CLASSES, 8, 1, false); break;                                                     \
+        case 112: HDC_SEARCH(CLASSES, 12, 1, false); break;                                                    \
+        case 116: HDC_SEARCH(CLASSES, 16, 1, false); break;                                                    \
+        case 212: HDC_SEARCH(CLASSES, 12, 2, false); break;                                                    \
+        case 216: HDC_SEARCH(CLASSES, 16, 2, false); break;                                                    \
+        case 412: HDC_SEARCH(CLASSES, 12, 4, false); break;                                                    \
+        default: HDC_SEARCH(CLASSES, 16, 4, false); break;                                                     \
+    }
+        if (form.share < kWaves) {
+            if (form.classes == 16) {
+                HDC_SEARCH_SHORT(16)
+            } else {
+                HDC_SEARCH_SHORT(32)
+            }
+            return;
+        }
+#undef HDC_SEARCH_SHORT
+    }
+    if (form.classes == 16) {
         switch (steps) {
-            case 4: HDC_SEARCH(16, 4, false); break;
-            case 8: HDC_SEARCH(16, 8, false); break;
-            case 12: HDC_SEARCH(16, 12, false); break;
-            case 16: HDC_SEARCH(16, 16, false); break;
-            case 20: HDC_SEARCH(16, 20, false); break;
-            default: HDC_SEARCH(16, 16, true); break;
+            case 4: HDC_SEARCH(16, 4, 8, false); break;
+            case 8: HDC_SEARCH(16, 8, 8, false); break;
+            case 12: HDC_SEARCH(16, 12, 8, false); break;
+            case 16: HDC_SEARCH(16, 16, 8, false); break;
+            case 20: HDC_SEARCH(16, 20, 8, false); break;
+            default: HDC_SEARCH(16, 16, 8, true); break;
         }
     } else {
         switch (steps) {
-            case 4: HDC_SEARCH(32, 4, false); break;
-            case 8: HDC_SEARCH(32, 8, false); break;
-            case 12: HDC_SEARCH(32, 12, false); break;
-            case 16: HDC_SEARCH(32, 16, false); break;
-            case 20: HDC_SEARCH(32, 20, false); break;
-            case 24: HDC_SEARCH(32, 24, false); break;
-            case 28: HDC_SEARCH(32, 28, false); break;
-            default: HDC_SEARCH(32, 16, true); break;
+            case 4: HDC_SEARCH(32, 4, 8, false); break;
+            case 8: HDC_SEARCH(32, 8, 8, false); break;
+            case 12: HDC_SEARCH(32, 12, 8, false); break;
+            case 16: HDC_SEARCH(32, 16, 8, false); break;
+            case 20: HDC_SEARCH(32, 20, 8, false); break;
+            case 24: HDC_SEARCH(32, 24, 8, false); break;
+            case 28: HDC_SEARCH(32, 28, 8, false); break;
+            default: HDC_SEARCH(32, 16, 8, true); break;
         }
     }
 #undef HDC_SEARCH
+}
+
+// Many samples of short rows: a row to as few waves as hold it in 16 steps, so that a block has up to eight tiles of samples at once.  us,
+// eight waves a row and so, nearest classes only; classes by samples of 1000 dimensions: 26 by 40000 (five tiles a compute unit) 11.2 13.6,
+// by 65000 13.6 10.7, by 1000000 160 54 (with cosines 165 89), 6 by 1000000 162 49; of 4096: 26 by 50000 15.9 15.4, 10 by 300000 69 46;
+// of 500: 26 by 1000000 132 42.  Long rows of up to 16 classes in blocks of 32, where a wave's share is not rounded up as far: 6 by
+// 200000 of 10000 74 and 60.
+Form form_of(const hdc_ctx_impl *c, int64_t tiles) {
+    const int classes = c->p.C > 16 ? 32 : 16;
+    if (tiles <= 6 * (int64_t)c->num_cus) return {classes, kWaves};
+    for (int share = 1; share < kWaves; share *= 2)
+        if (c->W <= share * (kWave / classes) * 16) return {classes, share};
+    return {32, kWaves};
 }
 
 }  // namespace
@@ -459,18 +535,20 @@ static int launch_nearest(hdc_ctx_impl *c, int64_t N, int splits, int32_t *pred,
 // wide: null, or by class whether its scales lie far apart: if none's do, the call has been answered.
 static int launch_search_few(hdc_ctx_impl *c, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
                              float *cos_out, int32_t *pred, const int *wide, hipStream_t s) {
-    const int groups = (c->p.C + kTile - 1) / kTile;
+    const int groups = (c->p.C + kTile - 1) / kTile;   // (of 16 classes there is one)
     const int64_t tiles = (N + kTile - 1) / kTile, cus = c->num_cus;
     // One block a compute unit.  One group of classes: as many tiles as that gives a block; more groups: the block walks over its tiles
     // for each, and where there are fewer tiles than compute units, the groups are split among blocks.
-    int64_t per = std::max<int64_t>(1, (tiles + cus - 1) / cus);
+    const Form form = form_of(c, tiles);
+    const int at_once = kWaves / form.share;
+    int64_t per = std::max<int64_t>(1, (tiles + cus - 1) / cus + at_once - 1) / at_once * at_once;
     if (groups > 1) per = std::min<int64_t>(per, kMaxTiles);
     const int splits_most = wide ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(groups, cus / tiles));
     const int of_split = (groups + splits_most - 1) / splits_most, splits = (groups + of_split - 1) / of_split;
     const int64_t blocks = (tiles + per - 1) / per, most = 1 << 22;   // blocks a launch
     for (int64_t b = 0; b < blocks; b += most) {
         const int64_t n0 = b * per * kTile, n = std::min(N - n0, most * per * kTile);
-        launch<kNearest>(c, dim3((unsigned)std::min(most, blocks - b), (unsigned)splits), s, hv + n0 * c->W, n, codes, scales, norm, (int)per, of_split, nullptr,
+        launch<kNearest>(c, form, dim3((unsigned)std::min(most, blocks - b), (unsigned)splits), s, hv + n0 * c->W, n, codes, scales, norm, (int)per, of_split, nullptr,
                          cos_out ? cos_out + n0 * c->p.C : nullptr, splits > 1 ? nullptr : pred + n0, c->qs_cos_d, c->qs_class_d, {}, wide);
     }
     HDC_HIP(hipGetLastError());
@@ -501,7 +579,7 @@ int launch_quantized_dots(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const
     *slices = 1;
     const int64_t tiles = (nb + kTile - 1) / kTile, groups = (c->p.C + kTile - 1) / kTile;
     const int64_t per = std::max<int64_t>(1, (tiles * groups + c->num_cus - 1) / c->num_cus);
-    launch<kDots>(c, dim3((unsigned)((tiles + per - 1) / per), (unsigned)groups), s, hv, nb, codes, scales, nullptr, (int)per, 1, part, nullptr, nullptr, nullptr,
+    launch<kDots>(c, {c->p.C > 16 ? 32 : 16, kWaves}, dim3((unsigned)((tiles + per - 1) / per), (unsigned)groups), s, hv, nb, codes, scales, nullptr, (int)per, 1, part, nullptr, nullptr, nullptr,
                  nullptr);
     HDC_HIP(hipGetLastError());
     return HDC_OK;
@@ -515,7 +593,7 @@ int launch_quantized_weights(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, co
                              hipStream_t s) {
     ProfScope prof(c, HDC_K_ONLINE_FWD, s);
     const int64_t tiles = out.ld / kTile, per = std::max<int64_t>(1, (tiles + c->num_cus - 1) / c->num_cus);
-    launch<kWeights>(c, dim3((unsigned)((tiles + per - 1) / per + out.tblocks)), s, hv, nb, codes, scales, nullptr, (int)per, 1, nullptr, nullptr, nullptr,
+    launch<kWeights>(c, {c->p.C > 16 ? 32 : 16, kWaves}, dim3((unsigned)((tiles + per - 1) / per + out.tblocks)), s, hv, nb, codes, scales, nullptr, (int)per, 1, nullptr, nullptr, nullptr,
                      nullptr, nullptr, out);
     HDC_HIP(hipGetLastError());
     return HDC_OK;

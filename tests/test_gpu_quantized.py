@@ -235,7 +235,26 @@ def test_cosines_of_many_samples_with_many_rows(N, C, D, kind):
     check_search(words(rng, N, D), x, want_cos=N != 3000)
 
 
-@pytest.mark.parametrize("N,C", [(17000, 70), (25000, 70), (8200, 300)])
+# very many samples of short rows: a row to one wave, two or four
+SHORT = [(50000, 3, 96), (50001, 10, 97), (49999, 26, 500), (50000, 16, 1025), (60001, 26, 700), (50017, 9, 2048), (50000, 20, 1500), (49200, 5, 3001),
+         (49160, 26, 2500), (50000, 40, 600), (66000, 64, 1000), (49153, 6, 4500)]
+
+
+@pytest.mark.parametrize("kind", ["normal", "zeros", "none", "orders"])
+@pytest.mark.parametrize("N,C,D", SHORT)
+def test_cosines_of_many_samples_with_short_rows(N, C, D, kind):
+    rng = np.random.default_rng(N + C * 3 + D * 11)
+    x = rows_of("normal" if kind == "none" else kind, C, D, rng)
+    if kind == "none":
+        x[1, D // 2], x[C - 1, 0] = np.nan, np.inf
+    if kind == "zeros":
+        x[C // 2] = 0
+    check_search(words(rng, N, D), x, want_cos=kind in ("none", "orders"))
+    if kind == "orders":
+        check_search(words(rng, N, D), x, want_cos=False)
+
+
+@pytest.mark.parametrize("N,C", [(17000, 70), (25000, 70), (8200, 300), (50000, 30), (50000, 14)])
 def test_equal_cosines_of_many_samples_go_to_the_lowest_class(N, C):
     """Rows that repeat, within a tile of classes and across, and multiples of one another by powers of two."""
     rng = np.random.default_rng(C)

@@ -260,8 +260,8 @@ int64_t search_many_limits() { return 2 * kMost; }
 
 // Whether a call goes this way, unless its rows' scales lie far apart: where the classes fill more than half of a block's and there are blocks
 // for three of eight compute units.  us, so and by search_quantized_kernel; classes by samples of 10000 dimensions: 64 by 64000 (250 blocks)
-// 72 49, 96 71 72, 128 74 93; 128 by 16000 (63) 62 43; 256 by 4000 (32) 61 36, by 16000 (126) 65 80; 1024 by 4000 (128) 70 123, by 64000 381
-// 652.  Of 1000: 64 by 64000 29 26, 96 29 39, 128 by 16000 19 23, 1024 by 1000 (32) 24 22, by 16000 35 152.
+// 67 47, 96 72 69, 128 67 85; 128 by 16000 (63) 60 41; 256 by 4000 (32) 59 36, by 16000 (126) 64 79; 1024 by 4000 (128) 66 124, by 64000 366
+// 627.  Of 1000: 64 by 64000 28 19, 96 27 26, 128 21 34; 256 by 4000 21 20, by 16000 22 39, 1024 by 16000 37 147.
 bool search_many_takes(const hdc_ctx_impl *c, int64_t N) {
     return c->p.C > kClasses / 2 && c->W >= kStep && (int64_t)c->W * kUnit * kClasses < ((int64_t)1 << 31) &&
            (N + kSamples - 1) / kSamples * ((c->p.C + kClasses - 1) / kClasses) >= c->num_cus * 3 / 8;

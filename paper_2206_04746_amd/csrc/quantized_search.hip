@@ -304,23 +304,38 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
             if (c_of == 0) keep(g, i * kTile + n_of, n, best);
         }
     };
-    // All of the tiles at once without their cosines: kLanes lanes a sample.
+    // All of the tiles at once, for the nearest class with kLanes lanes a sample; the cosines in the order in which they lie in memory if there are up
+    // to 16 (us, 1000000 samples of 1000, so and a tile at a time as where a row has all waves: 6 classes 57 77, 26 classes 91 89; 300000 of
+    // 4096, 26 classes 63 57).
     constexpr int kLanes = 16 / kAtOnce;
+    constexpr bool kLaidOut = kClasses == 16;
     auto finish_all = [&](int g, int i) {
+        const int64_t n0 = (tile0 + i * kAtOnce) * kTile;
+        auto cosine = [&](int at, int c) {
+            float sum = 0.0f;   // without rounding
+#pragma unroll
+            for (int w = 0; w < kShare; ++w) sum += sums[i & 1][at / kTile * kShare + w][c][at % kTile];
+            return (double)sum * ratio[c];
+        };
+        if (kLaidOut && cos_out) {
+            const int width = min(kClasses, C - g * kClasses), down = kThreads / width, right = kThreads % width;
+            for (int at = tid / width, c = tid % width; at < kAtOnce * kTile; at += down) {
+                if (n0 + at < N) cos_out[(n0 + at) * C + g * kClasses + c] = (float)cosine(at, c);
+                c += right;
+                if (c >= width) c -= width, ++at;
+            }
+        }
         const int at = tid / kLanes, lane_of = tid % kLanes;
         Best best = {-__builtin_inf(), kNoClass};
 #pragma unroll 4
         for (int c = lane_of; c < kClasses; c += kLanes) {
-            float sum = 0.0f;   // without rounding
-#pragma unroll
-            for (int w = 0; w < kShare; ++w) sum += sums[i & 1][at / kTile * kShare + w][c][at % kTile];
-            const double cs = (double)sum * ratio[c];
+            const double cs = cosine(at, c);
             if (cs > best.cos && g * kClasses + c < C) best = {cs, g * kClasses + c};
         }
         if constexpr (kLanes > 1) best = better(best, of_lane<0xB1>(best));
         if constexpr (kLanes > 2) best = better(best, of_lane<0x4E>(best));
         if constexpr (kLanes > 4) best = better(best, of_lane<0x141>(best));
-        if (lane_of == 0) keep(g, i * kAtOnce * kTile + at, (tile0 + i * kAtOnce) * kTile + at, best);
+        if (lane_of == 0) keep(g, i * kAtOnce * kTile + at, n0 + at, best);
     };
 
     constexpr int kEarly = kMode == kWeights ? 16 : 1;   // partial norms asked for first
@@ -365,7 +380,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
                 const int one = anew(1);   // (no loop of its own for the first tile)
                 for (int i = 0; i <= count; ++i) {
                     auto before = [&]() {
-                        if (kAtOnce > 1 && !cos_out) {
+                        if (kAtOnce > 1 && (kLaidOut || !cos_out)) {
                             finish_all(g, i - 1);
                             return;
                         }

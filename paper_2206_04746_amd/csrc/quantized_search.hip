@@ -465,9 +465,12 @@ __global__ __launch_bounds__(256) void nearest_kernel(const double *__restrict__
 
 // Classes of a block and the waves that share a row: for no more than 16 classes (v_mfma_scale_f32_16x16x128_f8f6f4) half of the loads and
 // registers (2947 samples of 10000 with 6 classes 6.9 us a call, in a block for 32 7.7; a batch of 64 in training 8.5 us, 8.9).
+// Rows that eight waves of either kind hold in four steps go in a block for 32 (batches of 32 samples of 1024, 5 classes: 10.4 us a batch, in a
+// block for 16 10.8).
 struct Form {
     int classes, share;
 };
+Form whole_block(const hdc_ctx_impl *c) { return {c->p.C > 16 || c->W <= 4 * kWaves * (kWave / 32) ? 32 : 16, kWaves}; }
 
 template <int kMode>
 void launch(hdc_ctx_impl *c, Form form, dim3 grid, hipStream_t s, const uint32_t *hv, int64_t N, const uint32_t *codes, const uint8_t *scales, const double *norm,
@@ -529,7 +532,7 @@ void launch(hdc_ctx_impl *c, Form form, dim3 grid, hipStream_t s, const uint32_t
 // 200000 of 10000 74 and 60.
 Form form_of(const hdc_ctx_impl *c, int64_t tiles) {
     const int classes = c->p.C > 16 ? 32 : 16;
-    if (tiles <= 6 * (int64_t)c->num_cus) return {classes, kWaves};
+    if (tiles <= 6 * (int64_t)c->num_cus) return whole_block(c);
     for (int share = 1; share < kWaves; share *= 2)
         if (c->W <= share * (kWave / classes) * 16) return {classes, share};
     return {32, kWaves};
@@ -594,7 +597,7 @@ int launch_quantized_dots(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const
     *slices = 1;
     const int64_t tiles = (nb + kTile - 1) / kTile, groups = (c->p.C + kTile - 1) / kTile;
     const int64_t per = std::max<int64_t>(1, (tiles * groups + c->num_cus - 1) / c->num_cus);
-    launch<kDots>(c, {c->p.C > 16 ? 32 : 16, kWaves}, dim3((unsigned)((tiles + per - 1) / per), (unsigned)groups), s, hv, nb, codes, scales, nullptr, (int)per, 1, part, nullptr, nullptr, nullptr,
+    launch<kDots>(c, whole_block(c), dim3((unsigned)((tiles + per - 1) / per), (unsigned)groups), s, hv, nb, codes, scales, nullptr, (int)per, 1, part, nullptr, nullptr, nullptr,
                  nullptr);
     HDC_HIP(hipGetLastError());
     return HDC_OK;
@@ -608,7 +611,7 @@ int launch_quantized_weights(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, co
                              hipStream_t s) {
     ProfScope prof(c, HDC_K_ONLINE_FWD, s);
     const int64_t tiles = out.ld / kTile, per = std::max<int64_t>(1, (tiles + c->num_cus - 1) / c->num_cus);
-    launch<kWeights>(c, {c->p.C > 16 ? 32 : 16, kWaves}, dim3((unsigned)((tiles + per - 1) / per + out.tblocks)), s, hv, nb, codes, scales, nullptr, (int)per, 1, nullptr, nullptr, nullptr,
+    launch<kWeights>(c, whole_block(c), dim3((unsigned)((tiles + per - 1) / per + out.tblocks)), s, hv, nb, codes, scales, nullptr, (int)per, 1, nullptr, nullptr, nullptr,
                      nullptr, nullptr, out);
     HDC_HIP(hipGetLastError());
     return HDC_OK;

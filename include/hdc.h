@@ -276,10 +276,11 @@ int hdc_dequantize(hdc_ctx *ctx, const uint32_t *codes_dev, const uint8_t *scale
 /*
  * hdc_search_cosine against quantised class rows v[C][D]: with s = 2*hv[n] - 1,
  *   cos[n][c] = <v[c], s> / (sqrt(norm[c]) * sqrt(D))   (0 where norm[c] is 0; fp64),
- *   pred[n]   = lowest c with the largest cos[n][c]     (compared in fp64; a cosine that is no number
- *               is below all others, class 0 if all are).
- * The products of 32 dimensions are whole numbers; their sums are formed without rounding where they
- * fit 24 bits and in fp64 otherwise.
+ *   pred[n]   = lowest c with the largest cos[n][c]     (compared as these quotients of fp64, whatever N; a
+ *               cosine that is no number is below all others, class 0 if all are).
+ * Dot products are whole multiples of half a row's smallest scale; their sums are formed without rounding where
+ * they fit 24 bits and in fp64 otherwise.  cos_dev takes a cosine rounded to fp32, formed as a product with a
+ * reciprocal in some calls (a rounding of fp64 more).
  *   hv_dev [N][W] (pad bits zero or not), codes_dev [C][W][4], scales_dev [C][W], norm_dev [C] as hdc_quantize
  *   leaves them, cos_dev [N][C] fp32 out or NULL, pred_dev [N] int32 out (required).
  */

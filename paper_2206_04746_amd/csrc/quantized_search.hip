@@ -73,7 +73,9 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     __shared__ int limits[2][kWaves][kTile];                    // largest and smallest scale of a class in a wave's dimensions
     __shared__ double run_cos[kMode == kNearest ? kMaxTiles * kTile : kTile];   // the nearest of the groups before; kWeights: norms of the classes
     __shared__ int run_c[kMode == kNearest ? kMaxTiles * kTile : 1];
-    __shared__ double ratio[kShare < kWaves ? kClasses : 1];    // unit by size
+    __shared__ double class_unit[kAtOnce > 1 ? kClasses : 1], class_size[kAtOnce > 1 ? kClasses : 1];   // unit and size by class of a group
+    __shared__ double ratio[kAtOnce > 1 ? kClasses : 1];        // unit by size, or 0
+    __shared__ float about[kAtOnce > 1 ? kClasses : 1];         // ... in fp32, no number for a class past the last
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, col = lane % kClasses, piece = lane / kClasses;
     if constexpr (kMode == kWeights) {
         const int idx = (int)blockIdx.x - ((int)gridDim.x - weigh.tblocks);
@@ -94,11 +96,12 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
     const int64_t all = kMode == kWeights ? weigh.ld / kTile : (N + kTile - 1) / kTile, tile0 = (int64_t)blockIdx.x * tiles;
     const int count = (int)((min((int64_t)tiles, all - tile0) + kAtOnce - 1) / kAtOnce), parts = kParts ? (W + kBlocks - 1) / kBlocks : 1;
     const int g0 = blockIdx.y * groups, g1 = min(g0 + groups, (C + kClasses - 1) / kClasses);
+    const bool several = kMode == kNearest && (g1 - g0 > 1 || !pred_out);   // groups whose nearest classes are compared
 
     v4u code[kSteps];
     uint32_t scale[kSteps / 4];   // a byte a step, less `top` (modulo 2^32, all four together): 127 for the row's largest
     int top = 0, passes = 1;      // the row's largest scale less 127; passes that the block needs
-    double unit[kOwn], size[kOwn];   // of this thread's classes: the largest scale; the row's norm times that of a sample (kNearest: 1 by it, or 0)
+    double unit[kOwn], size[kOwn];   // of this thread's classes: the largest scale; the row's norm times that of a sample
     const int n_of = tid >> 4, c_of = tid & 15;   // this thread's sample of a tile, and the first of its classes, which are 16 apart
     constexpr int kAhead = !kParts && kSteps <= 20 ? 1 : 0;   // words of the next sample asked for before this one's products, or after them
     uint32_t word[1 + kAhead][kCols][kSteps];
@@ -296,7 +299,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
 #pragma unroll
             for (int j = 0; j < kOwn; ++j)
                 if (c + 16 * j < C) {
-                    const double cs = total[j] * size[j];
+                    const double cs = size[j] == 0.0 ? 0.0 : total[j] / size[j];
                     if (cos_out && n < N) cos_out[n * C + c + 16 * j] = (float)cs;
                     best = better(best, Best{cs, c + 16 * j});
                 }
@@ -304,37 +307,60 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
             if (c_of == 0) keep(g, i * kTile + n_of, n, best);
         }
     };
-    // All of the tiles at once, for the nearest class with kLanes lanes a sample; the cosines in the order in which they lie in memory if there are up
-    // to 16 (us, 1000000 samples of 1000, so and a tile at a time as where a row has all waves: 6 classes 57 77, 26 classes 91 89; 300000 of
-    // 4096, 26 classes 63 57).
+    // All of the tiles at once, for the nearest class with kLanes lanes a sample.  The class is the one that the quotients in fp64 give, which are
+    // formed where fp32 does not tell them apart (its cosines are off by 2^-23 of themselves: the factor's rounding and the product's).
+    // Cosines in the order in which they lie in memory, but for blocks of 32 classes that take two tiles (us, so and a tile at a time as where a
+    // row has all waves: 26 classes, 1000000 samples of 1000 84 98, 300000 of 4096 - two tiles - 56 53; 20 classes, 400000 of 2000 46 51).
     constexpr int kLanes = 16 / kAtOnce;
-    constexpr bool kLaidOut = kClasses == 16;
+    constexpr bool kLaidOut = kClasses == 16 || kAtOnce > 2;
     auto finish_all = [&](int g, int i) {
         const int64_t n0 = (tile0 + i * kAtOnce) * kTile;
-        auto cosine = [&](int at, int c) {
+        auto sum_at = [&](int at, int c) {
             float sum = 0.0f;   // without rounding
 #pragma unroll
             for (int w = 0; w < kShare; ++w) sum += sums[i & 1][at / kTile * kShare + w][c][at % kTile];
-            return (double)sum * ratio[c];
+            return sum;
         };
+        auto quotient = [&](float sum, int c) { return class_size[c] == 0.0 ? 0.0 : (double)sum * class_unit[c] / class_size[c]; };
         if (kLaidOut && cos_out) {
             const int width = min(kClasses, C - g * kClasses), down = kThreads / width, right = kThreads % width;
             for (int at = tid / width, c = tid % width; at < kAtOnce * kTile; at += down) {
-                if (n0 + at < N) cos_out[(n0 + at) * C + g * kClasses + c] = (float)cosine(at, c);
+                if (n0 + at < N) cos_out[(n0 + at) * C + g * kClasses + c] = (float)((double)sum_at(at, c) * ratio[c]);
                 c += right;
                 if (c >= width) c -= width, ++at;
             }
         }
         const int at = tid / kLanes, lane_of = tid % kLanes;
-        Best best = {-__builtin_inf(), kNoClass};
+        float most = -__builtin_inff(), second = -__builtin_inff(), sum_of_most = 0.0f;   // the two largest
+        int which = kNoClass;
 #pragma unroll 4
-        for (int c = lane_of; c < kClasses; c += kLanes) {
-            const double cs = cosine(at, c);
-            if (cs > best.cos && g * kClasses + c < C) best = {cs, g * kClasses + c};
+        for (int c = lane_of; c < kClasses; c += kLanes) {   // (what is no number is neither above nor below)
+            const float sum = sum_at(at, c), v = sum * about[c];
+            const bool above = v > most;
+            second = above ? most : fmaxf(second, v);
+            most = above ? v : most, which = above ? c : which, sum_of_most = above ? sum : sum_of_most;
         }
-        if constexpr (kLanes > 1) best = better(best, of_lane<0xB1>(best));
-        if constexpr (kLanes > 2) best = better(best, of_lane<0x4E>(best));
-        if constexpr (kLanes > 4) best = better(best, of_lane<0x141>(best));
+        auto join = [&](auto sel) {
+            constexpr int kSel = decltype(sel)::value;
+            const float other = __uint_as_float(lanes<kSel>(__float_as_uint(most)));
+            const float sum = __uint_as_float(lanes<kSel>(__float_as_uint(sum_of_most)));
+            const int c = (int)lanes<kSel>((uint32_t)which);
+            second = fmaxf(fminf(most, other), fmaxf(second, __uint_as_float(lanes<kSel>(__float_as_uint(second)))));
+            const bool above = other > most || (other == most && c < which);
+            most = above ? other : most, which = above ? c : which, sum_of_most = above ? sum : sum_of_most;
+        };
+        if constexpr (kLanes > 1) join(std::integral_constant<int, kNext>{});
+        if constexpr (kLanes > 2) join(std::integral_constant<int, kNextPair>{});
+        if constexpr (kLanes > 4) join(std::integral_constant<int, kMirrorEight>{});
+        Best best = {-__builtin_inf(), kNoClass};
+        if (__builtin_expect(__ballot(second >= most * (1.0f - copysignf(0x1p-19f, most))) != 0, 0)) {
+            for (int c = lane_of; c < kClasses && g * kClasses + c < C; c += kLanes) best = better(best, Best{quotient(sum_at(at, c), c), g * kClasses + c});
+            if constexpr (kLanes > 1) best = better(best, of_lane<kNext>(best));
+            if constexpr (kLanes > 2) best = better(best, of_lane<kNextPair>(best));
+            if constexpr (kLanes > 4) best = better(best, of_lane<kMirrorEight>(best));
+        } else if (which != kNoClass) {
+            best = {several ? quotient(sum_of_most, which) : (double)most, g * kClasses + which};
+        }
         if (lane_of == 0) keep(g, i * kAtOnce * kTile + at, n0 + at, best);
     };
 
@@ -370,8 +396,11 @@ __global__ __launch_bounds__(kThreads, 2) void search_quantized_kernel(const uin
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) {
             size[j] = sqrt(size[j]) * root_d;
-            if constexpr (kMode == kNearest) size[j] = size[j] == 0.0 ? 0.0 : 1.0 / size[j];
-            if (kAtOnce > 1 && n_of == 0) ratio[c_of + 16 * j] = unit[j] * size[j];
+            if (kAtOnce > 1 && n_of == 0) {
+                const int c = c_of + 16 * j;
+                class_unit[c] = unit[j], class_size[c] = size[j], ratio[c] = size[j] == 0.0 ? 0.0 : unit[j] / size[j];
+                about[c] = g * kClasses + c < C ? (float)ratio[c] : __builtin_nanf("");
+            }
         }
         if constexpr (!kParts) {
             if (__builtin_expect(passes == 1, 1)) {

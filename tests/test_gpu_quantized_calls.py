@@ -1,0 +1,78 @@
+"""Calls with rows of 4-bit floats whose answer must not depend on the way that a call's size takes."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from oracle import quantized as oq  # noqa: E402
+
+from test_gpu_parity import dev_u32  # noqa: E402
+from test_gpu_quantized import U, context, quantized, rows_of, run_training, words  # noqa: E402
+
+
+def searched(hv, codes, scales, norm, C, D, want_cos):
+    """pred and cos (or None) on the host; tables on the device."""
+    ctx = context(D, C)
+    pred = torch.full((len(hv),), -7, dtype=torch.int32, device="cuda")
+    cos = torch.full((len(hv), C), 7.0, dtype=torch.float32, device="cuda") if want_cos else None
+    ctx.hdc_search_quantized(dev_u32(hv), codes, scales, norm, pred, cos)
+    torch.cuda.synchronize()
+    ctx.close()
+    return pred.cpu().numpy(), cos.cpu().numpy() if want_cos else None
+
+
+# ---- cosines that are equal by definition, or differ by one rounding: a row of 0, 1, 2 and 4 times 1.5 is as exact as itself, and its cosine
+# the same number but for the roundings of its norm's root, of the product with the sample's and of the quotient.  With whole numbers
+# for dot products and norms all that is rounded is what the definition rounds, so classes are equal to the oracle's whatever the call's size.
+def rows_of_multiples(C, D, rng, few=5):
+    x = rng.choice([0, 1, 2, 4], size=(C, D)) * rng.choice([-1, 1], size=(C, D))
+    x[:, ::32] = 4                                                     # (every block has the same scale)
+    x = x.astype(np.float64)
+    if C > few:
+        x[few:] = x[rng.integers(0, few, C - few)]
+    x *= rng.choice([1, 1.5], size=(C, 1)) * np.exp2(rng.integers(-3, 4, (C, 1)))
+    return x.astype(np.float32)
+
+
+@pytest.mark.parametrize("want_cos", [False, True])
+@pytest.mark.parametrize("N,C,D,far", [
+    (70, 10, 400, 0), (70, 30, 400, 0), (70, 40, 400, 0), (9, 300, 1000, 0), (600, 10, 10000, 0), (600, 30, 10000, 0),       # eight waves a row
+    (50000, 10, 400, 0), (50000, 30, 400, 0), (50000, 40, 400, 0), (50001, 12, 2048, 0), (50001, 20, 1500, 0),               # fewer waves a row
+    (17000, 100, 400, 0), (25000, 100, 400, 0), (8200, 300, 1021, 0),                                                                          # many classes
+    (40, 7, 20600, 0), (40, 20, 14500, 0),                                                                                     # rows in parts
+    (70, 10, 400, 12), (70, 40, 400, 12), (50000, 10, 400, 12), (17000, 100, 400, 12), (25000, 100, 400, 12), (40, 7, 20600, 12)])                    # scales far apart
+def test_classes_are_those_of_the_definition_whatever_the_size(N, C, D, far, want_cos):
+    rng = np.random.default_rng(N + C + D)
+    x = rows_of_multiples(C, D, rng)
+    if far:                                                            # half of the blocks 2^12 below the others: sums of 44 bits at most
+        x[:, np.arange(D) // 32 % 2 == 1] *= 2.0 ** -far
+    hv = words(rng, N, D)
+    codes, scales, norm = quantized(x)
+    v = oq.values(codes.cpu().numpy(), scales.cpu().numpy(), D)
+    assert np.array_equal(v, x)                                        # (nothing is rounded)
+    assert np.array_equal(norm.cpu().numpy(), (v * v).sum(1))
+    pred, _ = searched(hv, codes, scales, norm, C, D, want_cos)
+    for n in range(0, N, 4000):
+        assert np.array_equal(pred[n:n + 4000], oq.nearest(oq.cosines(hv[n:n + 4000], v, norm.cpu().numpy())))
+
+
+@pytest.mark.parametrize("N,C,D", [(300, 10, 400), (300, 30, 400), (300, 60, 400)])
+def test_training_scores_equal_cosines_as_the_search_does(N, C, D):
+    """One batch: the rows that it leaves tell which class was predicted (a wrong one loses about 1 at each of a sample's dimensions)."""
+    rng = np.random.default_rng(C)
+    x = rows_of_multiples(C, D, rng)
+    hv, y = words(rng, N, D), rng.integers(0, C, N).astype(np.int32)
+    codes, scales, norm = quantized(x)
+    pred, _ = searched(hv, codes, scales, norm, C, D, False)
+    got = run_training(hv, y, x, N, 1, 1.0)[0].astype(np.float64)
+    cos = oq.cosines(hv, x.astype(np.float64), norm.cpu().numpy())
+    weight = np.zeros((N, C))
+    at = np.arange(N)
+    weight[at, y] = (1.0 - cos[at, y]).astype(np.float32)
+    wrong = pred != y
+    weight[at[wrong], pred[wrong]] -= (1.0 - cos[at, pred]).astype(np.float32)[wrong]
+    want = (x + weight.T @ oq.signs(hv, D)).astype(np.float32)
+    # (a weight of at most 2 may be rounded the other way, an element once more)
+    assert np.all(np.abs(got - want) <= 2.0 ** -23 * np.abs(want) + 2.0 ** -23 * np.abs(weight).sum(0)[:, None])

@@ -43,7 +43,7 @@ constexpr int kFewWaves = 8;
 template <int kSize>
 __global__ __launch_bounds__(kFewWaves * kWave) void product_few_kernel(const uint32_t *__restrict__ a, const uint8_t *__restrict__ sa, int64_t M,
                                                                         const uint32_t *__restrict__ b, const uint8_t *__restrict__ sb, int64_t N, int W,
-                                                                        float *__restrict__ out) {
+                                                                        float *__restrict__ out, int64_t pitch) {
     constexpr int kGroups = kWave / kSize, kPerUnit = 4 * kGroups;   // lanes to a row, blocks of four instructions
     __shared__ float sums[kFewWaves][kSize][kSize + 1];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, waves = blockDim.x >> 6, col = lane % kSize, group = lane / kSize;
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void product_few_kernel(const ui
         const int r = at / kSize, k = at % kSize;
         double sum = 0.0;   // of the waves' fp32 sums, rounded once
         for (int w = 0; w < waves; ++w) sum += (double)sums[w][r][k];
-        if (m0 + r < M && n0 + k < N) out[(m0 + r) * N + n0 + k] = (float)sum;
+        if (m0 + r < M && n0 + k < N) out[(m0 + r) * pitch + n0 + k] = (float)sum;
     }
 }
 
@@ -305,11 +305,13 @@ int launch_product_quantized(hdc_ctx_impl *c, const uint32_t *a, const uint8_t *
     if (blocks(32) <= c->num_cus || W < 2 * kStep) {
         auto launch = [&](auto kernel, int size) {
             const int per = 4 * kWave / size, waves = std::min((W + per - 1) / per, kFewWaves);
-            for (int64_t m = 0; m < M; m += (int64_t)size * 65535) {
-                const int64_t rows = std::min<int64_t>(M - m, (int64_t)size * 65535);
-                hipLaunchKernelGGL(kernel, dim3((unsigned)((N + size - 1) / size), (unsigned)((rows + size - 1) / size)), dim3((unsigned)waves * kWave), 0, s,
-                                   a + m * W * 4, sa + m * W, rows, b, sb, N, W, out + m * N);
-            }
+            const int64_t most = (int64_t)size << 22;   // rows of b a launch, whose threads along x are fewer than 2^32 then
+            for (int64_t m = 0; m < M; m += (int64_t)size * 65535)
+                for (int64_t n = 0; n < N; n += most) {
+                    const int64_t rows = std::min<int64_t>(M - m, (int64_t)size * 65535), cols = std::min(N - n, most);
+                    hipLaunchKernelGGL(kernel, dim3((unsigned)((cols + size - 1) / size), (unsigned)((rows + size - 1) / size)), dim3((unsigned)waves * kWave), 0, s,
+                                       a + m * W * 4, sa + m * W, rows, b + n * W * 4, sb + n * W, cols, W, out + m * N + n, N);
+                }
         };
         if (blocks(16) <= c->num_cus)
             launch(product_few_kernel<16>, 16);

@@ -76,3 +76,27 @@ def test_training_scores_equal_cosines_as_the_search_does(N, C, D):
     want = (x + weight.T @ oq.signs(hv, D)).astype(np.float32)
     # (a weight of at most 2 may be rounded the other way, an element once more)
     assert np.all(np.abs(got - want) <= 2.0 ** -23 * np.abs(want) + 2.0 ** -23 * np.abs(weight).sum(0)[:, None])
+
+
+# ---- products of more rows than a launch has threads for
+def test_product_of_more_rows_than_a_launch_has_threads_for():
+    """2^31 + 70 rows of one dimension: 46 GB."""
+    N = (1 << 31) + 70
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("no room")
+    ctx = context(1)
+    codes, scales = torch.zeros((N, 4), dtype=torch.int32, device="cuda"), torch.full((N, 1), 127, dtype=torch.uint8, device="cuda")
+    codes[:, 0] = 4                                       # 2
+    codes[-100:, 0] = torch.arange(100, device="cuda", dtype=torch.int32) % 8
+    codes[:100, 0] = torch.arange(100, device="cuda", dtype=torch.int32) % 8 + 8
+    out = torch.full((1, N), -1.0, device="cuda")
+    ctx.hdc_product_quantized(codes[:1] * 0 + torch.tensor([[2, 0, 0, 0]], dtype=torch.int32, device="cuda"), scales[:1], codes, scales, out)
+    torch.cuda.synchronize()
+    ctx.close()
+    mags = torch.tensor(oq.MAGNITUDES, dtype=torch.float32, device="cuda")
+    at = torch.arange(100, device="cuda") % 8
+    assert torch.equal(out[0, :100], -mags[at]) and torch.equal(out[0, -100:], mags[at])
+    for n in range(100, N - 100, 1 << 28):
+        assert bool((out[0, n:min(n + (1 << 28), N - 100)] == 2.0).all())
+    del codes, scales, out
+    torch.cuda.empty_cache()

@@ -557,14 +557,15 @@ void launch(hdc_ctx_impl *c, Form form, dim3 grid, hipStream_t s, const uint32_t
 // Many samples of short rows: a row to as few waves as hold it in 16 steps, so that a block has up to eight tiles of samples at once.  us,
 // eight waves a row and so, nearest classes only; classes by samples of 1000 dimensions: 26 by 40000 (five tiles a compute unit) 11.2 13.6,
 // by 65000 13.6 10.7, by 1000000 160 54 (with cosines 165 89), 6 by 1000000 162 49; of 4096: 26 by 50000 15.9 15.4, 10 by 300000 69 46;
-// of 500: 26 by 1000000 132 42.  Long rows of up to 16 classes in blocks of 32, where a wave's share is not rounded up as far: 6 by
-// 200000 of 10000 74 and 60.
+// of 500: 26 by 1000000 132 42.  Longer rows of up to 16 classes in blocks of 32 while these hold them in 20 steps, with words ahead: a wave's
+// share is not rounded up as far.  In blocks of 16 and of 32, 6 classes: 200000 of 8500 56 54, of 10000 62 58, of 10240 63 55; of 10400 57 80,
+// 60000 of 12288 26 33, of 14336 31 33; in parts then, 60000 of 14400 30 82, of 20480 37 128.
 Form form_of(const hdc_ctx_impl *c, int64_t tiles) {
     const int classes = c->p.C > 16 ? 32 : 16;
     if (tiles <= 6 * (int64_t)c->num_cus) return whole_block(c);
     for (int share = 1; share < kWaves; share *= 2)
         if (c->W <= share * (kWave / classes) * 16) return {classes, share};
-    return {32, kWaves};
+    return c->W <= kWaves * (kWave / 32) * 20 ? Form{32, kWaves} : whole_block(c);
 }
 
 }  // namespace

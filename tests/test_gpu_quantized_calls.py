@@ -100,3 +100,62 @@ def test_product_of_more_rows_than_a_launch_has_threads_for():
         assert bool((out[0, n:min(n + (1 << 28), N - 100)] == 2.0).all())
     del codes, scales, out
     torch.cuda.empty_cache()
+
+# ---- long rows with so many samples that a block has several tiles of them: rows in parts, and rows that are held by one form of block only
+@pytest.mark.parametrize("kind", ["normal", "orders", "none"])
+@pytest.mark.parametrize("N,C,D", [(8230, 7, 20481), (8230, 20, 14337), (16420, 40, 14337), (49200, 7, 14400), (49200, 3, 20480), (49200, 5, 20481),
+                                   (49153, 12, 14336), (49200, 20, 14400),
+                                   (49200, 6, 10240), (49200, 6, 10241)])
+def test_long_rows_with_several_tiles_of_samples_a_block(N, C, D, kind):
+    """Cosines within their roundings (a sum of W whole numbers, W + 8 roundings of 2^-53, then the one to fp32) and the nearest class, of
+    the samples at the ends of the call and some hundreds between."""
+    rng = np.random.default_rng(N + C + D)
+    x = rows_of("normal" if kind == "none" else kind, C, D, rng)
+    if kind == "none":
+        x[1, D // 2] = np.nan
+    codes, scales, norm = quantized(x)
+    hv = words(rng, N, D)
+    pred, cos = searched(hv, codes, scales, norm, C, D, True)
+    v, norm = oq.values(codes.cpu().numpy(), scales.cpu().numpy(), D), norm.cpu().numpy()
+    assert pred.min() >= 0 and pred.max() < C
+    some = np.unique(np.concatenate([np.arange(70), np.arange(N - 70, N), rng.integers(0, N, 700)]))
+    want = oq.cosines(hv[some], v, norm)
+    slack = ((D + 31) // 32 + 8) * U
+    got = cos[some].astype(np.float64)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    ok = ~np.isnan(want)
+    assert np.all(np.abs(got - want)[ok] <= 2.0 ** -24 * np.abs(want)[ok] * (1 + 1e-6) + 1.5 * slack)
+    order = np.sort(np.where(np.isnan(want), -2, want), axis=1)
+    clear = order[:, -1] - order[:, -2] > 3 * slack
+    assert np.array_equal(pred[some][clear], oq.nearest(want)[clear])
+    # all others: as in calls of so few samples that a block has one tile of them
+    own = context(D, C)
+    for n in range(0, N, 4096):
+        few = torch.empty(min(4096, N - n), dtype=torch.int32, device="cuda")
+        of = torch.empty((len(few), C), device="cuda")
+        own.hdc_search_quantized(dev_u32(hv[n:n + 4096]), codes, scales, torch.from_numpy(norm).cuda(), few, of)
+        assert np.array_equal(few.cpu().numpy(), pred[n:n + 4096])
+        # (in as many parts as the form of the block has: the same number but for the last roundings)
+        assert np.allclose(of.cpu().numpy(), cos[n:n + 4096], rtol=2.0 ** -23, atol=3 * slack, equal_nan=True)
+    own.close()
+
+
+@pytest.mark.parametrize("N,C,D", [(8230, 7, 20481), (8230, 20, 14337)])
+def test_training_on_long_rows_with_several_tiles_of_samples_a_block(N, C, D):
+    rng = np.random.default_rng(N + C + D)
+    hv, y = words(rng, N, D), rng.integers(0, C, N).astype(np.int32)
+    acc = np.rint(30 * rng.normal(size=(C, D))).astype(np.float32)
+    got = run_training(hv, y, acc, N, 1, 0.5)[0]
+    _, _, v, norm = oq.quantize(acc)
+    total, size = np.zeros((C, D)), np.zeros(C)
+    for n in range(0, N, 1000):
+        h, of = hv[n:n + 1000], y[n:n + 1000]
+        cos = oq.cosines(h, v, norm)
+        pred, at, weight = oq.nearest(cos), np.arange(len(of)), np.zeros((len(of), C))
+        weight[at, of] = (1.0 - cos[at, of]).astype(np.float32)
+        wrong = pred != of
+        weight[at[wrong], pred[wrong]] = -(0.5 * (1.0 - cos[at, pred])).astype(np.float32)[wrong]
+        total += weight.T @ oq.signs(h, D)
+        size += np.abs(weight).sum(0)
+    want = (acc + total).astype(np.float32)
+    assert np.all(np.abs(got.astype(np.float64) - want) <= 2.0 ** -23 * np.abs(want) + 2.0 ** -23 * size[:, None])

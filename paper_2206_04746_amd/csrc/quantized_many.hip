@@ -264,7 +264,8 @@ int64_t search_many_limits() { return 2 * kMost; }
 // 67 47, 96 72 69, 128 67 85; 128 by 16000 (63) 60 41; 256 by 4000 (32) 59 36, by 16000 (126) 64 79; 1024 by 4000 (128) 66 124, by 64000 366
 // 627.  Of 1000: 64 by 64000 28 19, 96 27 26, 128 21 34; 256 by 4000 21 20, by 16000 22 39, 1024 by 16000 37 147.
 bool search_many_takes(const hdc_ctx_impl *c, int64_t N) {
-    return c->p.C > kClasses / 2 && c->W >= kStep && (int64_t)c->W * kUnit * kClasses < ((int64_t)1 << 31) &&
+    static_assert((int64_t)HDC_MAX_D / 32 * kUnit * kClasses < (int64_t)1 << 31, "places in a block's codes are of 32 bits");
+    return c->p.C > kClasses / 2 && c->W >= kStep &&
            (N + kSamples - 1) / kSamples * ((c->p.C + kClasses - 1) / kClasses) >= c->num_cus * 3 / 8;
 }
 

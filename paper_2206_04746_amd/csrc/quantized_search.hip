@@ -530,26 +530,28 @@ void launch(hdc_ctx_impl *c, Form form, dim3 grid, hipStream_t s, const uint32_t
         }
 #undef HDC_SEARCH_SHORT
     }
-    if (form.classes == 16) {
-        switch (steps) {
-            case 4: HDC_SEARCH(16, 4, 8, false); break;
-            case 8: HDC_SEARCH(16, 8, 8, false); break;
-            case 12: HDC_SEARCH(16, 12, 8, false); break;
-            case 16: HDC_SEARCH(16, 16, 8, false); break;
-            case 20: HDC_SEARCH(16, 20, 8, false); break;
-            default: HDC_SEARCH(16, 16, 8, true); break;
+    if constexpr (kMode != kDots) {   // (dot products of up to 32 classes become weights where they are formed)
+        if (form.classes == 16) {
+            switch (steps) {
+                case 4: HDC_SEARCH(16, 4, 8, false); break;
+                case 8: HDC_SEARCH(16, 8, 8, false); break;
+                case 12: HDC_SEARCH(16, 12, 8, false); break;
+                case 16: HDC_SEARCH(16, 16, 8, false); break;
+                case 20: HDC_SEARCH(16, 20, 8, false); break;
+                default: HDC_SEARCH(16, 16, 8, true); break;
+            }
+            return;
         }
-    } else {
-        switch (steps) {
-            case 4: HDC_SEARCH(32, 4, 8, false); break;
-            case 8: HDC_SEARCH(32, 8, 8, false); break;
-            case 12: HDC_SEARCH(32, 12, 8, false); break;
-            case 16: HDC_SEARCH(32, 16, 8, false); break;
-            case 20: HDC_SEARCH(32, 20, 8, false); break;
-            case 24: HDC_SEARCH(32, 24, 8, false); break;
-            case 28: HDC_SEARCH(32, 28, 8, false); break;
-            default: HDC_SEARCH(32, 16, 8, true); break;
-        }
+    }
+    switch (steps) {
+        case 4: HDC_SEARCH(32, 4, 8, false); break;
+        case 8: HDC_SEARCH(32, 8, 8, false); break;
+        case 12: HDC_SEARCH(32, 12, 8, false); break;
+        case 16: HDC_SEARCH(32, 16, 8, false); break;
+        case 20: HDC_SEARCH(32, 20, 8, false); break;
+        case 24: HDC_SEARCH(32, 24, 8, false); break;
+        case 28: HDC_SEARCH(32, 28, 8, false); break;
+        default: HDC_SEARCH(32, 16, 8, true); break;
     }
 #undef HDC_SEARCH
 }
@@ -627,7 +629,7 @@ int launch_quantized_dots(hdc_ctx_impl *c, const uint32_t *hv, int64_t nb, const
     *slices = 1;
     const int64_t tiles = (nb + kTile - 1) / kTile, groups = (c->p.C + kTile - 1) / kTile;
     const int64_t per = std::max<int64_t>(1, (tiles * groups + c->num_cus - 1) / c->num_cus);
-    launch<kDots>(c, whole_block(c), dim3((unsigned)((tiles + per - 1) / per), (unsigned)groups), s, hv, nb, codes, scales, nullptr, (int)per, 1, part, nullptr, nullptr, nullptr,
+    launch<kDots>(c, Form{32, kWaves}, dim3((unsigned)((tiles + per - 1) / per), (unsigned)groups), s, hv, nb, codes, scales, nullptr, (int)per, 1, part, nullptr, nullptr, nullptr,
                  nullptr);
     HDC_HIP(hipGetLastError());
     return HDC_OK;

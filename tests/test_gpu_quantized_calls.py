@@ -159,3 +159,28 @@ def test_training_on_long_rows_with_several_tiles_of_samples_a_block(N, C, D):
         size += np.abs(weight).sum(0)
     want = (acc + total).astype(np.float32)
     assert np.all(np.abs(got.astype(np.float64) - want) <= 2.0 ** -23 * np.abs(want) + 2.0 ** -23 * size[:, None])
+
+# ---- pad bits of samples may be set or not
+@pytest.mark.parametrize("kind", ["normal", "orders"])
+@pytest.mark.parametrize("N,C,D", [(1, 1, 1), (33, 6, 33), (70, 10, 1001), (70, 26, 4097), (40, 40, 777), (5, 300, 100), (50001, 10, 97), (50001, 26, 500),
+                                   (17000, 100, 290), (8200, 300, 1021), (40, 7, 20490), (40, 20, 14345)])
+def test_pad_bits_of_samples_count_for_nothing_in_a_search(N, C, D, kind):
+    rng = np.random.default_rng(N + C + D)
+    codes, scales, norm = quantized(rows_of(kind, C, D, rng))
+    hv = words(rng, N, D)
+    set_ = hv.copy()
+    set_[:, -1] |= rng.integers(0, 1 << 32, N, dtype=np.uint32) << np.uint32(D % 32)
+    assert D % 32 and (set_ != hv).any()
+    a, b = searched(hv, codes, scales, norm, C, D, True), searched(set_, codes, scales, norm, C, D, True)
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("N,C,D,batch", [(50, 3, 33, 20), (300, 26, 333, 300), (300, 40, 1001, 100), (1500, 20, 97, 1500), (20000, 6, 130, 20000), (70, 6, 20490, 40)])
+def test_pad_bits_of_samples_count_for_nothing_in_training(N, C, D, batch):
+    rng = np.random.default_rng(N + C + D)
+    hv, y = words(rng, N, D), rng.integers(0, C, N).astype(np.int32)
+    set_ = hv.copy()
+    set_[:, -1] |= rng.integers(0, 1 << 32, N, dtype=np.uint32) << np.uint32(D % 32)
+    acc = np.rint(10 * rng.normal(size=(C, D))).astype(np.float32)
+    for a, b in zip(run_training(hv, y, acc, batch, 1, 0.7), run_training(set_, y, acc, batch, 1, 0.7)):
+        assert np.array_equal(a, b)

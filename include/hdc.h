@@ -294,8 +294,10 @@ int hdc_search_quantized(hdc_ctx *ctx, const uint32_t *hv_dev, int64_t N, const 
  *   a_codes_dev [M][W][4], a_scales_dev [M][W], b_codes_dev [N][W][4], b_scales_dev [N][W],
  *   out_dev [M][N] fp32 out.  M == 0 or N == 0 is a successful no-op.  a and b may be the same rows.
  * A sum is of eight or fewer fp32 sums where it is short of rows, of one otherwise: without rounding where
- * it and what it adds fit 24 bits.  Products of two blocks below 2^-126 may count as 0, sums beyond fp32 are
- * infinite, and what a block that is no number takes part in is no number.
+ * it and what it adds fit 24 bits.  Products of two blocks below 2^-126 may count as 0.  A product whose partial
+ * sums leave fp32 may be infinite, or no number where two of them do with different signs, also if it would fit
+ * itself; none can where the magnitudes of its terms add up to less than fp32's largest number.  What a block
+ * that is no number takes part in is no number.
  */
 int hdc_product_quantized(hdc_ctx *ctx, const uint32_t *a_codes_dev, const uint8_t *a_scales_dev, int64_t M,
                           const uint32_t *b_codes_dev, const uint8_t *b_scales_dev, int64_t N, float *out_dev,

@@ -184,3 +184,57 @@ def test_pad_bits_of_samples_count_for_nothing_in_training(N, C, D, batch):
     acc = np.rint(10 * rng.normal(size=(C, D))).astype(np.float32)
     for a, b in zip(run_training(hv, y, acc, batch, 1, 0.7), run_training(set_, y, acc, batch, 1, 0.7)):
         assert np.array_equal(a, b)
+
+# ---- products whose partial sums leave fp32: infinite or no number, never a number that is wrong
+PRODUCTS = [(10, 30, 600), (300, 200, 600), (30, 40, 300), (600, 600, 513), (1290, 1300, 769), (3000, 3000, 512)]
+
+
+@pytest.mark.parametrize("M,N,D", PRODUCTS)
+@pytest.mark.parametrize("signs", ["equal", "mixed", "halves"])
+def test_products_beyond_fp32_are_infinite_or_no_number(M, N, D, signs):
+    """Blocks around 2^62 on both sides: sums of magnitudes between far below and far beyond 2^128.  (halves: b's first dimensions are positive,
+    the others negative, so that partial sums leave fp32 both ways.)"""
+    rng = np.random.default_rng(M + N + D)
+
+    def rows(n, halves=False):
+        x = rng.normal(size=(n, D)) if signs == "mixed" else np.abs(rng.normal(size=(n, D)))
+        x[:, D // 2:] *= -1 if halves else 1
+        return (x * np.exp2(rng.integers(54, 64, (n, 1)))).astype(np.float32)
+    ctx = context(D)
+    a, sa, _ = quantized(rows(M), ctx, norm=False)
+    b, sb, _ = quantized(rows(N, signs == "halves"), ctx, norm=False)
+    out = torch.full((M, N), 3.0, device="cuda")
+    ctx.hdc_product_quantized(a, sa, b, sb, out)
+    torch.cuda.synchronize()
+    ctx.close()
+    va, vb = oq.values(a.cpu().numpy(), sa.cpu().numpy(), D), oq.values(b.cpu().numpy(), sb.cpu().numpy(), D)
+    got, want, size = out.cpu().numpy().astype(np.float64), va @ vb.T, np.abs(va) @ np.abs(vb).T
+    slack = (D + 2) * 2.0 ** -24 * size
+    number = np.isfinite(got)
+    assert np.all(np.abs(got - want)[number] <= slack[number])                  # what is a number is right
+    fits = size * (1 + (D + 2) * 2.0 ** -24) < 2.0 ** 128 - 2.0 ** 103
+    assert np.all(number[fits]) and fits.any() and (~fits).any()                # and where no partial sum can leave fp32 it is one
+    beyond = ~number & ~np.isnan(got)
+    assert np.all(size[beyond] >= 2.0 ** 127)
+    if signs == "equal":
+        assert not np.isnan(got).any() and np.all(got[want - slack > 2.0 ** 128] == np.inf)
+
+
+@pytest.mark.parametrize("M,N,D", PRODUCTS)
+@pytest.mark.parametrize("run", [32, 1])
+def test_zeros_beside_huge_values_add_nothing(M, N, D, run):
+    """Of every two runs of dimensions (blocks, or single ones) a has huge values in the first and b in the second; the last block has products of 1
+    on every dimension."""
+    W = (D + 31) // 32
+    x, y = np.zeros((M, D), np.float32), np.zeros((N, D), np.float32)
+    block = np.arange(D) // 32
+    x[:, np.arange(D) // run % 2 == 0], y[:, np.arange(D) // run % 2 == 1] = 3.0e38, -3.0e38
+    x[:, block == W - 1] = y[:, block == W - 1] = 1.0
+    ctx = context(D)
+    a, sa, _ = quantized(x, ctx, norm=False)
+    b, sb, _ = quantized(y, ctx, norm=False)
+    out = torch.full((M, N), 3.0, device="cuda")
+    ctx.hdc_product_quantized(a, sa, b, sb, out)
+    torch.cuda.synchronize()
+    ctx.close()
+    assert bool((out == float((block == W - 1).sum())).all())

@@ -1,8 +1,11 @@
 // Cosine inference with class rows of 4-bit floats, for many samples and many classes (arXiv 2206.04746, Sec. III): a block takes
-// 128 classes and 256 samples, 256 dimensions at a time.  The codes go through LDS, the steps after next on their way while one is
-// multiplied; a wave's samples are 64 of the 256, whose words it turns into +-1 itself (7 instructions for 32 dimensions, for
-// 128 classes).  So of both sides together a step loads 24 KB for 17 MFLOP, and matrix instructions are what bounds it:
-// 16001 samples of 8191 dimensions by 1024 classes take 103 us, 2.6 PFLOP/s, 64000 of 10000 366 us, 3.6.
+// 128 classes and 256 samples, 256 dimensions at a time.  The codes go through LDS, with room for three steps; a wave's samples are 64 of
+// the 256, whose words it turns into +-1 itself (7 instructions for 32 dimensions, for 128 classes), so that of both sides together a step
+// loads 24 KB for 17 MFLOP.  16001 samples of 8191 dimensions by 1024 classes take 103 us, 2.6 PFLOP/s, 64000 of 10000 366 us, 3.6.
+// Matrix instructions are 29 of the 103 us (28 % of the active cycles, at 2.3 GHz).  What bounds it is a step's latency: scales come by
+// ordinary loads, and before it takes or asks for them the compiler waits for all that the two waves that bring them have on their
+// way, the latest loads into LDS too, for which the other two waves then wait at the barrier.  After the loop 53 registers a lane are spilled (216
+// bytes of scratch; 28 MB of the 95 that such a call writes).
 //
 // The sums are of fp32, over the whole row, and without rounding: whole multiples of half the row's smallest scale, at most 192
 // of its largest for a block.  scan_kernel finds out whether every row's scales lie near enough to one another for that; if
@@ -163,7 +166,7 @@ __global__ __launch_bounds__(kThreads, 2) void search_many_kernel(const uint32_t
     };
 
     // At the end of a step its buffer takes the third step from it (past the row, the last ones again), and no more than these loads are on their
-    // way when the next step begins.
+    // way when the next step begins (of the waves that bring scales none).
     constexpr int kLoads = kClasses / 32 + kB;
     static_assert(kLoads == 6, "what is waited for");
     auto meet = [&]() {
@@ -259,10 +262,14 @@ __global__ __launch_bounds__(kThreads, 2) void search_many_kernel(const uint32_t
 
 int64_t search_many_limits() { return 2 * kMost; }
 
-// Whether a call goes this way, unless its rows' scales lie far apart: where the classes fill more than half of a block's and there are blocks
-// for three of eight compute units.  us, so and by search_quantized_kernel; classes by samples of 10000 dimensions: 64 by 64000 (250 blocks)
-// 67 47, 96 72 69, 128 67 85; 128 by 16000 (63) 60 41; 256 by 4000 (32) 59 36, by 16000 (126) 64 79; 1024 by 4000 (128) 66 124, by 64000 366
-// 627.  Of 1000: 64 by 64000 28 19, 96 27 26, 128 21 34; 256 by 4000 21 20, by 16000 22 39, 1024 by 16000 37 147.
+// Whether a call goes this way, unless its rows' scales lie far apart: where the classes fill more than half of a block's (of its first: the
+// rule does not look at how many are left for the last) and there are blocks for three of eight compute units.  us, so and by
+// search_quantized_kernel; classes by samples of 10000 dimensions: 64 by 64000 (250 blocks) 67 47, 96 68 72, 128 67 91; 128 by 16000 (63) 60 41;
+// 256 by 4000 (32) 59 36, by 16000 (126) 67 78; 1024 by 4000 (128) 66 124, by 64000 366 627.  Of 1000: 64 by 64000 28 19, 96 22 29, 128 29 36;
+// 256 by 4000 21 20, by 16000 29 40, 1024 by 16000 37 147.
+// Just past 128 the second block's classes are few, and the rule is wrong by up to a fifth, of calls of 16000 by a quarter: of 10000, 129 by
+// 16000 63 49, by 64000 95 105, by 200000 309 260; 160 63 51, 97 107, 319 266; 192 63 60, 101 128, 321 313; 257 by 16000 67 84, by 200000 498
+// 465; 320 507 526.  Of 1000, 129 by 400000 153 142, 192 152 178, 257 216 256.  96 by 200000 of 10000 179 173.
 bool search_many_takes(const hdc_ctx_impl *c, int64_t N) {
     static_assert((int64_t)HDC_MAX_D / 32 * kUnit * kClasses < (int64_t)1 << 31, "places in a block's codes are of 32 bits");
     return c->p.C > kClasses / 2 && c->W >= kStep &&

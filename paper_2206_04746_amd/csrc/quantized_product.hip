@@ -3,8 +3,9 @@
 //
 // Many rows: tiles of a's rows by b's rows through LDS, 256 dimensions at a time (128 bytes a row, loaded straight into LDS), the next step's
 // while a step's are multiplied; within a step a wave takes the operands of its next matrix instructions while it issues these.
-// 8191 by 4093 rows of 9999: 219 us, 3.06 PFLOP/s, of which matrix instructions on such data are 150 (at the clock that they leave the chip); loads
-// take the rest where a row is no whole number of cache lines (8192 by 4096: of 9999 245, of 9984 187).
+// 8191 by 4093 rows of 9999: 219 us, 3.06 PFLOP/s.  Matrix instructions are 82 us of that (38 % of the active cycles, at the 2.1 GHz that they leave
+// the chip): a step waits for its loads and reads of LDS, with which they overlap in part only.  Where a row is no whole number of
+// cache lines loads take longer (8192 by 4096: of 9999 245, of 9984 187; without loads 175 and, without scales, too, 154).
 // Few rows: a block takes 32 by 32 rows, or 16 by 16 (v_mfma_scale_f32_16x16x128_f8f6f4), its waves a share of the dimensions each, without LDS
 // but for the sum over the waves.
 #include <algorithm>

@@ -5,12 +5,14 @@
 // an eighth of the dimensions and holds the codes of its classes there in registers, so that all there is to read on the way is the
 // samples, once.  The waves' parts of the dot products meet in LDS.  Where a row is short and samples are many, four, two or one of
 // the waves hold it, and the block takes two, four or eight times 32 samples at once, for one barrier and with fewer lanes a sample at the end.
-// 200000 samples of 10000 dimensions, 26 classes: 65 us (3.9 TB/s of words), 1000000 of 1000: 54.
+// 200000 samples of 10000 dimensions, 26 classes: 64 us (3.9 TB/s of words), with the launch 67; 1000000 of 1000: 51, with cosines 83.
 //
 // Sums without rounding: the products of a row are whole multiples of half its smallest scale, and a block of 32 dimensions gives at
 // most 192 (32 times 6) of the largest.  Where a row's scales lie no further apart than 2^kRange, sums over it fit the 24 bits of
 // fp32, the waves' and theirs together.  Where they lie further apart, the blocks are taken in several passes, each of the scales
-// that lie within such a range, and the passes are added in fp64.
+// that lie within such a range, and the passes are added in fp64.  (us, rows of
+// normal values, and with blocks up to 2^12 and 2^24 smaller: 200000 samples of 10000, 26 classes 61 132 211; 1000000 of 1000 46 125
+// 150; 16001 of 8191, 1024 classes, which go by the other kernel only as the first, 86 415 605.)
 #include <algorithm>
 #include <type_traits>
 
@@ -557,9 +559,9 @@ void launch(hdc_ctx_impl *c, Form form, dim3 grid, hipStream_t s, const uint32_t
 }
 
 // Many samples of short rows: a row to as few waves as hold it in 16 steps, so that a block has up to eight tiles of samples at once.  us,
-// eight waves a row and so, nearest classes only; classes by samples of 1000 dimensions: 26 by 40000 (five tiles a compute unit) 11.2 13.6,
-// by 65000 13.6 10.7, by 1000000 160 54 (with cosines 165 89), 6 by 1000000 162 49; of 4096: 26 by 50000 15.9 15.4, 10 by 300000 69 46;
-// of 500: 26 by 1000000 132 42.  Longer rows of up to 16 classes in blocks of 32 while these hold them in 20 steps, with words ahead: a wave's
+// eight waves a row and so, nearest classes only; classes by samples of 1000 dimensions: 26 by 40000 (five tiles a compute unit) 11.4 10.5,
+// by 65000 14.6 10.7, by 1000000 142 49 (with cosines 152 83), 6 by 1000000 128 39; of 4096: 26 by 50000 15.5 16.0, 10 by 300000 54 37;
+// of 500: 26 by 1000000 137 38.  Longer rows of up to 16 classes in blocks of 32 while these hold them in 20 steps, with words ahead: a wave's
 // share is not rounded up as far.  In blocks of 16 and of 32, 6 classes: 200000 of 8500 56 54, of 10000 62 58, of 10240 63 55; of 10400 57 80,
 // 60000 of 12288 26 33, of 14336 31 33; in parts then, 60000 of 14400 30 82, of 20480 37 128.
 Form form_of(const hdc_ctx_impl *c, int64_t tiles) {

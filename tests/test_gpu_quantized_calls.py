@@ -40,6 +40,7 @@ def rows_of_multiples(C, D, rng, few=5):
 @pytest.mark.parametrize("N,C,D,far", [
     (70, 10, 400, 0), (70, 30, 400, 0), (70, 40, 400, 0), (9, 300, 1000, 0), (600, 10, 10000, 0), (600, 30, 10000, 0),       # eight waves a row
     (50000, 10, 400, 0), (50000, 30, 400, 0), (50000, 40, 400, 0), (50001, 12, 2048, 0), (50001, 20, 1500, 0),               # fewer waves a row
+    (50000, 6, 5000, 0), (50000, 26, 2500, 0), (50000, 40, 2500, 0), (50000, 26, 2500, 12),                                    # ... four of them
     (17000, 100, 400, 0), (25000, 100, 400, 0), (8200, 300, 1021, 0),                                                                          # many classes
     (40, 7, 20600, 0), (40, 20, 14500, 0),                                                                                     # rows in parts
     (70, 10, 400, 12), (70, 40, 400, 12), (50000, 10, 400, 12), (17000, 100, 400, 12), (25000, 100, 400, 12), (40, 7, 20600, 12)])                    # scales far apart
